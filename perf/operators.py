@@ -196,11 +196,14 @@ class _Grid:
         self.first = first
 
 
-def _quantise(x):
-    """Blocks [n, 16, h, d] in fp32 -> whole numbers and the largest magnitude [n, 1, h, 1]."""
+def _quantise(x, dtype=None):
+    """Blocks [n, 16, h, d] in fp32 -> whole numbers and the largest magnitude [n, 1, h, 1].  The quotient of 16-bit numbers is never
+    so close to half a step that 32 bits would round it the other way; that of 32-bit numbers is formed in 64."""
     a = x.abs().amax(dim=(1, 3), keepdim=True)
-    q = torch.round(x * 127.0 / torch.where(a > 0, a, torch.ones_like(a)))
-    return q, a
+    div = torch.where(a > 0, a, torch.ones_like(a))
+    if dtype is torch.float32:
+        return torch.round(x.double() * 127.0 / div.double()).float(), a
+    return torch.round(x * 127.0 / div), a
 
 
 def _fill(x, grid):
@@ -212,7 +215,7 @@ def _fill(x, grid):
 def _store(x, grid):
     """Tokens -> their blocks as the cache holds them: int8 numbers, magnitudes, and the tokens themselves (open blocks)."""
     b = _fill(x, grid)
-    q, a = _quantise(b)
+    q, a = _quantise(b, x.dtype)
     return q.to(torch.int8), a, b.to(x.dtype)
 
 
@@ -309,7 +312,7 @@ def _plain_write(case, s):
         if s["reopen"]:
             frm, to = s["reopen"]
             b.view((-1,) + b.shape[2:])[to] = s["cache"][c][2].view((-1,) + b.shape[2:])[frm].float()
-        q, a = _quantise(b)
+        q, a = _quantise(b, s[name].dtype)
         blocks = _held(q, a, b, grid.full)
         if "cache" in s:
             blocks = torch.cat([_held(*s["cache"][c], s["cache_grid"].full), blocks])
@@ -498,15 +501,19 @@ def exact(case, seed):
     new, old, h, d, n_q = x["new"], x["old"], case["n_kv"], case["d"], case["n_q"]
     per = n_q // h
 
-    def blocks(t):
-        """Tokens [n, heads, d] from position 0 on -> what the cache holds of them."""
+    def units(t):
+        """Tokens [n, heads, d] from position 0 on -> 127 times what the cache holds of them: whole numbers times the block's
+        largest magnitude, exact in 64 bits, so that a number on half a step is seen to be there when it is rounded again."""
         t = t.double()
         shut = t.shape[0] // 16 * 16
         b = t[:shut].reshape(-1, 16, t.shape[1], d)
         top = b.abs().max(dim=3)[0].max(dim=1)[0][:, None, :, None]
         # rounded to the nearest, halves to even, as torch.round does
         whole = torch.round(torch.where(top == 0, torch.zeros_like(b), b * 127 / top))
-        return torch.cat([(whole * top / 127).reshape(shut, t.shape[1], d), t[shut:]])
+        return torch.cat([(whole * top).reshape(shut, t.shape[1], d), t[shut:] * 127])
+
+    def blocks(t):
+        return units(t) / 127
 
     def cached(sq, o0, n0):
         ks, vs = [], []
@@ -533,10 +540,10 @@ def exact(case, seed):
                     mark[:, n - recent:] = True
                     pos = torch.nonzero(mark)[:, 1].view(h, keep)
                 for name in ("k", "v"):
-                    held = blocks(x[name][layer][n0:n0 + n])
+                    held = units(x[name][layer][n0:n0 + n])
                     if n > keep:
-                        held = torch.stack([held[pos[g], g] for g in range(h)], dim=1)
-                        held = blocks(held)
+                        held = units(torch.stack([held[pos[g], g] for g in range(h)], dim=1)) / 127
+                    held = held / 127
                     out.append(held.permute(1, 0, 2).reshape(-1))
                 wk.append(torch.stack([w[g, pos[g]] for g in range(h)]).double().reshape(-1))
             wts += wk
