@@ -230,6 +230,60 @@ int ss_kv_export_dev(ss_ctx*, const ss_shard_desc*, const int64_t* seq_ids, int 
 int ss_kv_import_dev(ss_ctx*, const ss_shard_desc*, const int64_t* seq_ids, const int32_t* lens, int n,
                      const void* staging, void* stream);
 
+/* ---- KV caches in 8 bits ---------------------------------------------------
+ * The KV store bounds how many sequences decode at once (paper section 4.2, b_max in Appendix A.3), and its bytes
+ * bound a decode step.  A shard can keep its pages in 8 bits: half the store, half the bytes.
+ *
+ * A block is 16 consecutive cached tokens of one kv head, K and V apart: one page's share of a head.  A full block whose
+ * largest magnitude is A holds the whole numbers q = v * 127 / A, rounded to the nearest, halves to even, and stands
+ * for q * (A / 127).  (A = 0: zeros.  A block with a value that is not finite stands for NaN throughout.)  The
+ * last block of a sequence, its open block, is kept in the model dtype as well and is read from there until it is
+ * full, so what the cache holds depends on the tokens alone, not on how they came.  Attention, export, swap-out and
+ * ss_kv_read see what the blocks stand for, the last three rounded once to the model dtype.
+ *
+ * ss_kv8_enable: the descriptor's pages are kept in 8 bits from now on; before its first use (SS_EINVAL once it has
+ *   pages).  gpu_kv_pages pages as before, of half the size (fp32: a quarter).  max_seqs: sequences resident at
+ *   once, an open block each (2 * heads * 16 * head_dim elements per layer); SS_ENOMEM for more.  weights != 0: the
+ *   shard keeps an attention weight per token and kv head, for ss_kv8_evict.
+ *
+ * On such a shard the layer calls, ss_kv_swap, ss_kv_reshard, the device-side export / import and the offline loop work as
+ * described at each, with these differences: the calls that bring tokens append.  kv_lens_before[i] has to
+ * be the layer's number of tokens of that sequence, or to cut the cache back: to a multiple of 16, or to a place inside
+ * the block its last tokens went to (a step may be repeated); SS_EINVAL otherwise.  A sequence is listed once per batch.
+ * Calls on a capturing stream are refused (SS_EHIP): a graph would hold the page lists of now.  They wait on
+ * the host for queued movements of their sequences.
+ *
+ * ss_kv8_write: the batch's keys and values, already rotated, into `layer` of the cache.
+ * ss_kv8_attn_prefill: writes qkv->k and qkv->v like ss_kv8_write, then out [T, n_q * head_dim] = causal attention of
+ *   qkv->q over what the cache holds: the query at position p sees positions 0 .. p, query head a the kv head
+ *   a / (n_q / n_kv) of the shard's, scores are divided by sqrt(head_dim).  With k and v both NULL nothing is
+ *   written: the tokens have to be there.
+ * ss_kv8_attn_decode: the same, one token per sequence, which adds the softmax weights of all query heads of a kv
+ *   head to the weights of the tokens they fell on, if the shard keeps them (prefill does not).
+ *   q, k, v: device, model dtype, 16-byte aligned; tokens *_stride elements apart (a multiple of 16 bytes), heads
+ *   back to back, so that they may be parts of one fused row.  out must not overlap them.
+ * ss_kv8_weights: the accumulated weights of whole sequences out of (SS_OUT) or into (SS_IN) buf, device,
+ *   [seq][layer_local][head_local][token], sequences back to back.  Newly written or imported tokens have weight 0.
+ * ss_kv8_evict: cuts every listed sequence of more than keep[i] tokens to keep[i] (>= 1), in every layer and kv head on its own: the
+ *   `recent` newest tokens stay (all keep[i] if recent is larger), of the others those of greatest weight, the
+ *   earlier of equal ones; NaN counts as greatest.  They keep their order and weights and are put into blocks anew
+ *   (rounded once more, in 32-bit arithmetic, those that end in the open block to the model dtype).  Pages that are no longer needed return
+ *   to the pool.  Batches go on counting positions: kv_lens_before of the next token is what it would be without the
+ *   eviction, and may not lie before it.  An evicted sequence is not swapped out (SS_EINVAL), its positions would be
+ *   lost; ss_kv_seq_len and the export count cached tokens.  All layers have to hold the same number of tokens.
+ */
+typedef struct { int32_t max_seqs, weights; } ss_kv8_cfg;
+typedef struct {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;     /* elements */
+} ss_qkv;
+int ss_kv8_enable(ss_ctx*, const ss_shard_desc*, const ss_kv8_cfg*);
+int ss_kv8_write(ss_ctx*, const ss_shard_desc*, int layer, const ss_batch*, const ss_qkv*, void* stream);
+int ss_kv8_attn_prefill(ss_ctx*, const ss_shard_desc*, int layer, const ss_batch*, const ss_qkv*, void* out, void* stream);
+int ss_kv8_attn_decode(ss_ctx*, const ss_shard_desc*, int layer, const ss_batch*, const ss_qkv*, void* out, void* stream);
+int ss_kv8_weights(ss_ctx*, const ss_shard_desc*, int dir, const int64_t* seq_ids, int n, float* buf, void* stream);
+int ss_kv8_evict(ss_ctx*, const ss_shard_desc*, const int64_t* seq_ids, const int32_t* keep, int n, int recent, void* stream);
+
 /* ---- inspection (tests) ------------------------------------------------ */
 /* pages [*n_inout] receives the page ids of seq; *n_inout returns the count. */
 int ss_kv_page_table(ss_ctx*, const ss_shard_desc*, int64_t seq, int32_t* pages, int32_t* n_inout);

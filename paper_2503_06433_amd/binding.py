@@ -59,6 +59,15 @@ class _LayerWeights(C.Structure):
 _lib = None
 
 
+class Kv8Cfg(C.Structure):
+    _fields_ = [("max_seqs", C.c_int32), ("weights", C.c_int32)]
+
+
+class _Qkv(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
+
+
 class OfflineCfg(C.Structure):
     _fields_ = [("prefill", ShardDesc), ("decode", ShardDesc), ("max_prefill_tokens", C.c_int32),
                 ("max_decode_seqs", C.c_int32), ("reshard_weights", C.c_int32), ("swap_in_group", C.c_int32)]
@@ -104,6 +113,12 @@ def load_library():
         "ss_host_tier_release": (I, [V, P(L), I]),
         "ss_kv_export_dev": (I, [V, D, P(L), I, V, V]),
         "ss_kv_import_dev": (I, [V, D, P(L), P(C.c_int32), I, V, V]),
+        "ss_kv8_enable": (I, [V, D, P(Kv8Cfg)]),
+        "ss_kv8_write": (I, [V, D, I, P(_Batch), P(_Qkv), V]),
+        "ss_kv8_attn_prefill": (I, [V, D, I, P(_Batch), P(_Qkv), V, V]),
+        "ss_kv8_attn_decode": (I, [V, D, I, P(_Batch), P(_Qkv), V, V]),
+        "ss_kv8_weights": (I, [V, D, I, P(L), I, V, V]),
+        "ss_kv8_evict": (I, [V, D, P(L), P(C.c_int32), I, I, V]),
         "ss_kv_page_table": (I, [V, D, L, P(C.c_int32), P(C.c_int32)]),
         "ss_kv_seq_len": (I, [V, D, L, P(C.c_int32)]),
         "ss_kv_read": (I, [V, D, L, I, V]),
@@ -132,6 +147,7 @@ def load_library():
 EXPORTED = ("ss_create ss_destroy ss_last_error ss_load_layer ss_host_weights_put ss_reshard_weights ss_weights_wait "
             "ss_weights_shard_bytes ss_weights_read ss_layer_prefill ss_layer_decode ss_layers_prefill ss_layers_decode ss_kv_swap "
             "ss_kv_reshard ss_sync ss_kv_jobs_issued ss_kv_wait ss_kv_free ss_host_tier_release ss_kv_export_dev ss_kv_import_dev "
+            "ss_kv8_enable ss_kv8_write ss_kv8_attn_prefill ss_kv8_attn_decode ss_kv8_weights ss_kv8_evict "
             "ss_kv_page_table ss_kv_seq_len ss_kv_read ss_host_tier_read ss_host_tier_used_bytes "
             "ss_kv_free_pages ss_load_head ss_embed ss_lm_head ss_lm_head_noalloc ss_get_config ss_offline_run ss_prof_enable ss_prof_read ss_prof_reset").split()
 
@@ -148,6 +164,16 @@ def _ptr(x):
     if isinstance(x, np.ndarray):
         return x.ctypes.data
     return x.data_ptr()
+
+
+def _rows(x, width):
+    """Address and row stride, in elements, of [tokens, heads, d] or [tokens, heads * d] with the heads back to back."""
+    if x is None:
+        return None, 0
+    row = x[0] if x.shape[0] else x.new_empty(x.shape[1:])
+    if row.numel() != width or not row.is_contiguous():
+        raise ValueError("rows of %d elements expected, heads back to back, not %s with strides %s" % (width, tuple(x.shape), x.stride()))
+    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else width
 
 
 def _i64(a):
@@ -303,6 +329,60 @@ class Context:
         s, l = _i64(seq_ids), _i32(lens)
         self._ck(self.lib.ss_kv_import_dev(self.h, C.byref(desc), s.ctypes.data_as(C.POINTER(C.c_int64)),
                                            l.ctypes.data_as(C.POINTER(C.c_int32)), len(s), _ptr(staging), stream))
+
+    # ---- caches in 8 bits
+    def _heads(self, desc):
+        k = desc.k if desc.mode == SS_TP else 1
+        return self.model.n_q_heads // k, self.model.n_kv_heads // k
+
+    def _qkv(self, desc, q, k, v, tokens):
+        n_q, n_kv = self._heads(desc)
+        d = self.model.head_dim
+        code = {"torch.float32": SS_F32, "torch.bfloat16": SS_BF16, "torch.float16": SS_F16}
+        for x in (q, k, v):
+            if x is not None and (x.shape[0] != tokens or code.get(str(x.dtype)) != self.model.dtype or x.device.index != self.runtime.device):
+                raise ValueError("%d tokens of the model's type on its device expected, not %s of %s on %s" %
+                                 (tokens, tuple(x.shape), x.dtype, x.device))
+        (qp, qs), (kp, ks), (vp, vs) = _rows(q, n_q * d), _rows(k, n_kv * d), _rows(v, n_kv * d)
+        return _Qkv(qp, kp, vp, qs, ks, vs)
+
+    def _attn_out(self, desc, q, out):
+        n_q, _ = self._heads(desc)
+        if out.numel() != q.shape[0] * n_q * self.model.head_dim or out.dtype != q.dtype or not out.is_contiguous() or out.device != q.device:
+            raise ValueError("out: %d contiguous elements of %s on %s expected" % (q.shape[0] * n_q * self.model.head_dim, q.dtype, q.device))
+        return _ptr(out)
+
+    def kv8_enable(self, desc, max_seqs, weights=False):
+        self._ck(self.lib.ss_kv8_enable(self.h, C.byref(desc), C.byref(Kv8Cfg(max_seqs, int(weights)))))
+
+    def kv8_write(self, desc, layer, seq_ids, q_lens, kv_before, k, v, stream=0):
+        """k, v: torch tensors [tokens, heads, d] (or the heads flat), tokens any stride apart."""
+        bt, keep = self._batch(seq_ids, q_lens, kv_before)
+        qkv = self._qkv(desc, None, k, v, int(keep[1].sum()))
+        self._ck(self.lib.ss_kv8_write(self.h, C.byref(desc), layer, C.byref(bt), C.byref(qkv), stream))
+
+    def kv8_attn_prefill(self, desc, layer, seq_ids, q_lens, kv_before, q, k, v, out, stream=0):
+        """k = v = None: their tokens are in the cache already."""
+        bt, keep = self._batch(seq_ids, q_lens, kv_before)
+        qkv = self._qkv(desc, q, k, v, int(keep[1].sum()))
+        self._ck(self.lib.ss_kv8_attn_prefill(self.h, C.byref(desc), layer, C.byref(bt), C.byref(qkv), self._attn_out(desc, q, out), stream))
+
+    def kv8_attn_decode(self, desc, layer, seq_ids, kv_before, q, k, v, out, stream=0):
+        bt, keep = self._batch(seq_ids, np.ones(len(seq_ids), dtype=np.int32), kv_before)
+        qkv = self._qkv(desc, q, k, v, len(keep[1]))
+        self._ck(self.lib.ss_kv8_attn_decode(self.h, C.byref(desc), layer, C.byref(bt), C.byref(qkv), self._attn_out(desc, q, out), stream))
+
+    def kv8_weights(self, desc, direction, seq_ids, buf, stream=0):
+        """buf: float32 on the device, [sequence][layer][head][token] back to back."""
+        s = _i64(seq_ids)
+        self._ck(self.lib.ss_kv8_weights(self.h, C.byref(desc), direction, s.ctypes.data_as(C.POINTER(C.c_int64)), len(s), _ptr(buf), stream))
+
+    def kv8_evict(self, desc, seq_ids, keep, recent, stream=0):
+        s, k = _i64(seq_ids), _i32(keep)
+        if len(s) != len(k):
+            raise ValueError("%d sequences, %d lengths to keep" % (len(s), len(k)))
+        self._ck(self.lib.ss_kv8_evict(self.h, C.byref(desc), s.ctypes.data_as(C.POINTER(C.c_int64)),
+                                       k.ctypes.data_as(C.POINTER(C.c_int32)), len(s), recent, stream))
 
     # ---- inspection
     def kv_page_table(self, desc, seq):

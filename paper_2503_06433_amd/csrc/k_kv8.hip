@@ -1,0 +1,565 @@
+// Cache in 8 bits: what fills it, reads it back, keeps the accumulated attention weights and evicts by them.  Everything here moves
+// data: bound by HBM.  The arithmetic of a block (see Kv8Layer): A = max |v|, q = rint(v * 127 / A).  The product v * 127 is exact
+// for 16-bit v and the quotient is correctly rounded; a quotient of two numbers of up to 11 bits is never closer to half a
+// step than 2^-12 without being on it, the error of the fp32 quotient is at most 2^-18: q is the one of real arithmetic.  For 32-bit v
+// a quotient that close to half a step is formed again in 64 bits (25 bits decide there).
+#include "ss_device.h"
+#include "ss_kernels.h"
+
+namespace SS_NS {
+using namespace ssk;
+
+// Where 127 times a value would pass the largest float both sides of the quotient are scaled; a power of two leaves it as it is.
+__device__ __forceinline__ float kv8_fit(float amax) { return amax > 1e36f ? 0.00390625f : 1.f; }
+template <typename T> __device__ __forceinline__ int kv8_round(float v, float amax) {
+    if (!(amax > 0.f && amax < INFINITY)) return 0;
+    const float t = v * 127.f / amax, r = rintf(t);
+    if (sizeof(T) == 4 && fabsf(t - r) > 0.499f) return (int)rint((double)v * 127.0 / (double)amax);
+    return (int)r;
+}
+__device__ __forceinline__ float kv8_step(float amax) { return amax / 127.f; }
+// a value that is not finite makes the block's magnitude NaN, and no other way round (fmaxf would drop a NaN)
+__device__ __forceinline__ float kv8_mag(float v) { const float a = fabsf(v); return a < INFINITY ? a : INFINITY; }
+__device__ __forceinline__ float kv8_amax(float m) { return m < INFINITY ? m : __uint_as_float(0x7fc00000u); }
+
+__device__ __forceinline__ uint32_t kv8_pack4(const int* q) {
+    return (uint32_t)(q[0] & 255) | (uint32_t)(q[1] & 255) << 8 | (uint32_t)(q[2] & 255) << 16 | (uint32_t)(q[3] & 255) << 24;
+}
+__device__ __forceinline__ int kv8_byte(uint32_t w, int i) { return (int)(int8_t)(w >> (8 * i)); }
+
+// One wave's share of a block of 16 tokens x D elements: lane l has rows 4 * (l / 16) + i, i = 0 .. 3, and of each the 16-byte
+// pieces l % 16, l % 16 + 16, ... (one or two, half the lanes idle where a row has only 8 pieces).  Four tokens of one element are
+// then in one lane: a dword of the transposed V page.
+template <typename T, int D> struct Kv8Tile {
+    static constexpr int EV = 16 / (int)sizeof(T);
+    static constexpr int PIECES = D / EV;                       // 16-byte pieces of a row: 8, 16 or 32
+    static constexpr int NP = PIECES > 16 ? PIECES / 16 : 1;
+    float x[4][NP * EV];
+    __device__ static bool idle(int lane) { return PIECES < 16 && (lane & 15) >= PIECES; }
+    __device__ static int col(int lane, int p) { return ((lane & 15) + 16 * p) * EV; }
+};
+
+// LDS image of a V page, 4 tokens a dword: element e, tokens 4 * r .. + 3.  Rows of 8 elements are padded so that what 16 lanes
+// write falls on all banks.
+__device__ __forceinline__ int kv8_vword(int e, int r) { return e * 4 + r + (e >> 3) * 4; }
+template <int D> constexpr int kv8_vwords = D * 4 + (D / 8) * 4;
+
+// Quantises the tile into K rows and, through `lds` (kv8_vwords of this wave), V rows.
+template <typename T, int D>
+__device__ __forceinline__ void kv8_store_block(const Kv8Tile<T, D>& k, const Kv8Tile<T, D>& v, int8_t* kp, int8_t* vp, float* amax,
+                                                uint32_t* lds, int lane) {
+    using Tile = Kv8Tile<T, D>;
+    float mk = 0.f, mv = 0.f;
+    if (!Tile::idle(lane)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < Tile::NP * Tile::EV; ++e) {
+                mk = fmaxf(mk, kv8_mag(k.x[i][e]));
+                mv = fmaxf(mv, kv8_mag(v.x[i][e]));
+            }
+    }
+    mk = wave_max(mk);
+    mv = wave_max(mv);
+    if (lane == 0) {
+        amax[0] = kv8_amax(mk);
+        amax[1] = kv8_amax(mv);
+    }
+    const float fk = kv8_fit(mk), fv = kv8_fit(mv), ak = mk * fk, av = mv * fv;
+    if (!Tile::idle(lane)) {
+#pragma unroll
+        for (int p = 0; p < Tile::NP; ++p) {
+            const int c = Tile::col(lane, p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int e = 0; e < Tile::EV; e += 4) {
+                    int q[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) q[j] = kv8_round<T>(k.x[i][p * Tile::EV + e + j] * fk, ak);
+                    *reinterpret_cast<uint32_t*>(kp + (4 * (lane >> 4) + i) * D + c + e) = kv8_pack4(q);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < Tile::EV; ++e) {
+                int q[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q[i] = kv8_round<T>(v.x[i][p * Tile::EV + e] * fv, av);
+                lds[kv8_vword(c + e, lane >> 4)] = kv8_pack4(q);
+            }
+        }
+    }
+    __builtin_amdgcn_wave_barrier();
+    __threadfence_block();
+#pragma unroll
+    for (int r = 0; r < D / 64; ++r) {
+        const int e = r * 64 + lane;
+        vec16 o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.w[i] = lds[kv8_vword(e, i)];
+        *reinterpret_cast<vec16*>(vp + e * 16) = o;
+    }
+}
+
+// rows [0, slot0) of the open block, then cnt rows of src
+template <typename T, int D>
+__device__ __forceinline__ void kv8_load_tile(Kv8Tile<T, D>& t, const T* src, int64_t stride, const T* open, int slot0, int lane) {
+    using Tile = Kv8Tile<T, D>;
+    if (Tile::idle(lane)) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = 4 * (lane >> 4) + i;
+        const T* p = row < slot0 ? open + row * D : src + (row - slot0) * stride;
+#pragma unroll
+        for (int j = 0; j < Tile::NP; ++j) unpack16<T>(*reinterpret_cast<const vec16*>(p + Tile::col(lane, j)), t.x[i] + j * Tile::EV);
+    }
+}
+
+// n rows of D elements into the open block from slot `at` on
+template <typename T, int D>
+__device__ __forceinline__ void kv8_copy_rows(const T* src, int64_t stride, T* open, int at, int n, int lane) {
+    constexpr int EV = 16 / (int)sizeof(T), PIECES = D / EV;
+    for (int i = lane; i < n * PIECES; i += 64)
+        *reinterpret_cast<vec16*>(open + (at + i / PIECES) * D + i % PIECES * EV) =
+            *reinterpret_cast<const vec16*>(src + (i / PIECES) * stride + i % PIECES * EV);
+}
+
+// New tokens.  One wave per (page unit, kv head): a unit is the tokens of a sequence that fall into one block.  A unit that
+// fills its block quantises it.  The tokens of a sequence's last block go to its open block; the wave of the sequence's FIRST unit
+// brings them there, because that unit may begin inside the block that was open before and has to read that one first.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv8_write_kernel(const T* k, int64_t k_stride, const T* v, int64_t v_stride, int n_heads,
+                                                        Kv8Batch b, Kv8Layer kv) {
+    __shared__ uint32_t lds[4][kv8_vwords<D>];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t id = (int64_t)blockIdx.x * 4 + wave;
+    if (id >= (int64_t)b.n_units * n_heads) return;
+    const int u = (int)(id / n_heads), g = (int)(id % n_heads);
+    const int sq = b.unit_seq[u], tok0 = b.unit_tok0[u], pos0 = b.unit_pos0[u], cnt = b.unit_cnt[u];
+    const int before = b.before[sq], end = b.end[sq];
+    const size_t page = (size_t)b.page_tables[(size_t)sq * b.pt_stride + pos0 / 16] * n_heads + g;
+    T* ko = (T*)kv.open + ((size_t)b.slot[sq] * 2 * n_heads + g) * 16 * D;
+    T* vo = ko + (size_t)n_heads * 16 * D;
+    const int slot0 = pos0 & 15;
+    k += (size_t)g * D;
+    v += (size_t)g * D;
+    if (kv.w && lane < cnt) kv.w[page * 16 + slot0 + lane] = 0.f;
+    if (slot0 + cnt == 16) {
+        Kv8Tile<T, D> tk, tv;
+        kv8_load_tile<T, D>(tk, k + tok0 * k_stride, k_stride, ko, slot0, lane);
+        kv8_load_tile<T, D>(tv, v + tok0 * v_stride, v_stride, vo, slot0, lane);
+        kv8_store_block<T, D>(tk, tv, kv.k + page * 16 * D, kv.v + page * 16 * D, kv.amax + page * 2, lds[wave], lane);
+    }
+    if (pos0 == before) {
+        const int last = (end - 1) & ~15, from = last > before ? last : before, n = end - from;
+        const int64_t t = (int64_t)b.cu_q[sq] + from - before;
+        kv8_copy_rows<T, D>(k + t * k_stride, k_stride, ko, from & 15, n, lane);
+        kv8_copy_rows<T, D>(v + t * v_stride, v_stride, vo, from & 15, n, lane);
+    }
+}
+
+// Whole sequences from staging [K | V][head][position][D]: a wave per (page, unit, head).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv8_scatter_kernel(const Kv8Layer* __restrict__ layers, int n_heads, RepackUnits u,
+                                                          const T* __restrict__ staging) {
+    __shared__ uint32_t lds[4][kv8_vwords<D>];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int unit = blockIdx.y, g = blockIdx.z, pg = blockIdx.x * 4 + wave, len = u.unit_len[unit];
+    if (pg * 16 >= len) return;
+    const Kv8Layer kv = layers[u.unit_layer[unit]];
+    const size_t page = (size_t)u.pages[u.unit_pt[unit] + pg] * n_heads + g;
+    const T* k = staging + u.unit_off[unit] + ((size_t)g * len + pg * 16) * D;
+    const T* v = k + (size_t)n_heads * len * D;
+    const int n = len - pg * 16 < 16 ? len - pg * 16 : 16;
+    if (kv.w && lane < n) kv.w[page * 16 + lane] = 0.f;
+    if (n == 16) {
+        Kv8Tile<T, D> tk, tv;
+        kv8_load_tile<T, D>(tk, k, D, nullptr, 0, lane);
+        kv8_load_tile<T, D>(tv, v, D, nullptr, 0, lane);
+        kv8_store_block<T, D>(tk, tv, kv.k + page * 16 * D, kv.v + page * 16 * D, kv.amax + page * 2, lds[wave], lane);
+    }
+    if (pg * 16 + n == len) {
+        T* ko = (T*)kv.open + ((size_t)u.unit_slot[unit] * 2 * n_heads + g) * 16 * D;
+        kv8_copy_rows<T, D>(k, D, ko, 0, n, lane);
+        kv8_copy_rows<T, D>(v, D, ko + (size_t)n_heads * 16 * D, 0, n, lane);
+    }
+}
+
+// ... and into it: full blocks as what they stand for, rounded once to the model's type, the open block as it is.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv8_gather_kernel(const Kv8Layer* __restrict__ layers, int n_heads, RepackUnits u,
+                                                         T* __restrict__ staging) {
+    using Tile = Kv8Tile<T, D>;
+    __shared__ uint32_t lds[4][kv8_vwords<D>];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int unit = blockIdx.y, g = blockIdx.z, pg = blockIdx.x * 4 + wave, len = u.unit_len[unit];
+    if (pg * 16 >= len) return;
+    const Kv8Layer kv = layers[u.unit_layer[unit]];
+    T* k = staging + u.unit_off[unit] + ((size_t)g * len + pg * 16) * D;
+    T* v = k + (size_t)n_heads * len * D;
+    const int n = len - pg * 16;
+    if (n < 16) {
+        const T* ko = (const T*)kv.open + ((size_t)u.unit_slot[unit] * 2 * n_heads + g) * 16 * D;
+        kv8_copy_rows<T, D>(ko, D, k, 0, n, lane);
+        kv8_copy_rows<T, D>(ko + (size_t)n_heads * 16 * D, D, v, 0, n, lane);
+        return;
+    }
+    const size_t page = (size_t)u.pages[u.unit_pt[unit] + pg] * n_heads + g;
+    const int8_t *kp = kv.k + page * 16 * D, *vp = kv.v + page * 16 * D;
+    const float sk = kv8_step(kv.amax[page * 2]), sv = kv8_step(kv.amax[page * 2 + 1]);
+    uint32_t* l = lds[wave];
+#pragma unroll
+    for (int r = 0; r < D / 64; ++r) {
+        const vec16 w = *reinterpret_cast<const vec16*>(vp + (r * 64 + lane) * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l[kv8_vword(r * 64 + lane, i)] = w.w[i];
+    }
+    __builtin_amdgcn_wave_barrier();
+    __threadfence_block();
+    if (Tile::idle(lane)) return;
+#pragma unroll
+    for (int p = 0; p < Tile::NP; ++p) {
+        const int c = Tile::col(lane, p);
+        uint32_t vw[Tile::EV];
+#pragma unroll
+        for (int e = 0; e < Tile::EV; ++e) vw[e] = l[kv8_vword(c + e, lane >> 4)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = 4 * (lane >> 4) + i;
+            float f[Tile::EV];
+#pragma unroll
+            for (int e = 0; e < Tile::EV; e += 4) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(kp + row * D + c + e);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f[e + j] = (float)kv8_byte(w, j) * sk;
+            }
+            *reinterpret_cast<vec16*>(k + row * D + c) = pack16<T>(f);
+#pragma unroll
+            for (int e = 0; e < Tile::EV; ++e) f[e] = (float)kv8_byte(vw[e], i) * sv;
+            *reinterpret_cast<vec16*>(v + row * D + c) = pack16<T>(f);
+        }
+    }
+}
+
+#define SS_TYPED(dt, d, KERNEL, ...)                                        \
+    do {                                                                    \
+        if ((dt) == F32) {                                                  \
+            if ((d) == 64) KERNEL<float, 64> __VA_ARGS__;                   \
+            else KERNEL<float, 128> __VA_ARGS__;                            \
+        } else {                                                            \
+            if ((d) == 64) KERNEL<bf16_t, 64> __VA_ARGS__;                  \
+            else KERNEL<bf16_t, 128> __VA_ARGS__;                           \
+        }                                                                   \
+    } while (0)
+
+template <typename T, int D>
+static void launch_write(const void* k, int64_t ks, const void* v, int64_t vs, int n_heads, const Kv8Batch& b, const Kv8Layer& kv, hipStream_t s) {
+    const long long waves = (long long)b.n_units * n_heads;
+    kv8_write_kernel<T, D><<<(unsigned)((waves + 3) / 4), 256, 0, s>>>((const T*)k, ks, (const T*)v, vs, n_heads, b, kv);
+}
+
+hipError_t kv8_write(int dt, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int n_heads, int d, const Kv8Batch& b,
+                     const Kv8Layer& kv, hipStream_t s) {
+    if (b.n_units <= 0) return hipSuccess;
+    const int ev = dt == F32 ? 4 : 8;
+    if ((d != 64 && d != 128) || n_heads <= 0 || (long long)b.n_units * n_heads > 0x7fffffffll) return hipErrorInvalidValue;
+    if (((uintptr_t)k | (uintptr_t)v) % 16 || k_stride % ev || v_stride % ev) return hipErrorInvalidValue;
+    SS_TYPED(dt, d, launch_write, (k, k_stride, v, v_stride, n_heads, b, kv, s));
+    return hipGetLastError();
+}
+
+template <typename T, int D>
+static void launch_gather(const Kv8Layer* layers, int n_heads, const RepackUnits& u, void* staging, dim3 grid, hipStream_t s) {
+    kv8_gather_kernel<T, D><<<grid, 256, 0, s>>>(layers, n_heads, u, (T*)staging);
+}
+template <typename T, int D>
+static void launch_scatter(const Kv8Layer* layers, int n_heads, const RepackUnits& u, const void* staging, dim3 grid, hipStream_t s) {
+    kv8_scatter_kernel<T, D><<<grid, 256, 0, s>>>(layers, n_heads, u, (const T*)staging);
+}
+
+static bool repack_fits(int n_heads, int d, const RepackUnits& u) {
+    return (d == 64 || d == 128) && n_heads > 0 && n_heads <= 65535 && u.n_units <= 65535 && u.unit_slot;
+}
+
+hipError_t kv8_gather(int dt, const Kv8Layer* layers, int n_heads, int d, const RepackUnits& u, void* staging, hipStream_t s) {
+    if (u.n_units <= 0 || u.max_pages <= 0) return hipSuccess;
+    if (!repack_fits(n_heads, d, u)) return hipErrorInvalidValue;
+    SS_TYPED(dt, d, launch_gather, (layers, n_heads, u, staging, dim3((u.max_pages + 3) / 4, u.n_units, n_heads), s));
+    return hipGetLastError();
+}
+
+hipError_t kv8_scatter(int dt, const Kv8Layer* layers, int n_heads, int d, const RepackUnits& u, const void* staging, hipStream_t s) {
+    if (u.n_units <= 0 || u.max_pages <= 0) return hipSuccess;
+    if (!repack_fits(n_heads, d, u)) return hipErrorInvalidValue;
+    SS_TYPED(dt, d, launch_scatter, (layers, n_heads, u, staging, dim3((u.max_pages + 3) / 4, u.n_units, n_heads), s));
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- rotary embedding of a batch's q and k, in place
+// A thread per (token, head, 16-byte piece of the first half): it has the pairs of both halves.
+template <typename T>
+__global__ __launch_bounds__(256) void kv8_rope_kernel(T* __restrict__ qkv, int heads, int64_t row_stride, int d, const float* __restrict__ rope,
+                                                       Kv8Batch b) {
+    constexpr int V = VecOf<T>::N;
+    const int u = blockIdx.x, sq = b.unit_seq[u], cnt = b.unit_cnt[u];
+    const int pos0 = b.unit_pos0[u] - b.before[sq] + b.pos[sq];
+    const int cph = d / 2 / V;
+    for (int i = threadIdx.x; i < cnt * heads * cph; i += 256) {
+        const int c = i % cph * V, h = i / cph % heads, t = i / (cph * heads);
+        T* lo_p = qkv + (size_t)(b.unit_tok0[u] + t) * row_stride + (size_t)h * d + c;
+        T* hi_p = lo_p + d / 2;
+        const float* cs = rope + (size_t)(pos0 + t) * d + 2 * c;
+        float lo[V], hi[V], olo[V], ohi[V];
+        unpack16<T>(*reinterpret_cast<const vec16*>(lo_p), lo);
+        unpack16<T>(*reinterpret_cast<const vec16*>(hi_p), hi);
+#pragma unroll
+        for (int j = 0; j < V; ++j) rope_rotate(lo[j], hi[j], cs[2 * j], cs[2 * j + 1], olo[j], ohi[j]);
+        *reinterpret_cast<vec16*>(lo_p) = pack16<T>(olo);
+        *reinterpret_cast<vec16*>(hi_p) = pack16<T>(ohi);
+    }
+}
+
+hipError_t kv8_rope(int dt, void* qkv, int n_q, int n_kv, int d, const float* rope_table, const Kv8Batch& b, hipStream_t s) {
+    if (b.n_units <= 0) return hipSuccess;
+    if (d % 16 || n_q <= 0 || n_kv <= 0) return hipErrorInvalidValue;
+    const int64_t stride = (int64_t)(n_q + 2 * n_kv) * d;
+    if (dt == F32) kv8_rope_kernel<float><<<b.n_units, 256, 0, s>>>((float*)qkv, n_q + n_kv, stride, d, rope_table, b);
+    else kv8_rope_kernel<bf16_t><<<b.n_units, 256, 0, s>>>((bf16_t*)qkv, n_q + n_kv, stride, d, rope_table, b);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- accumulated weights of whole sequences
+__global__ __launch_bounds__(256) void kv8_weights_kernel(const Kv8Layer* __restrict__ layers, int n_heads, RepackUnits u, float* __restrict__ buf,
+                                                          bool in) {
+    const int unit = blockIdx.y, len = u.unit_len[unit], t = blockIdx.x * 256 + threadIdx.x;
+    if (t >= len) return;
+    float* w = layers[u.unit_layer[unit]].w + ((size_t)u.pages[u.unit_pt[unit] + t / 16] * n_heads) * 16 + t % 16;
+    float* p = buf + u.unit_off[unit] + t;
+    for (int g = blockIdx.z; g < n_heads; g += gridDim.z) {
+        if (in) w[(size_t)g * 16] = p[(size_t)g * len];
+        else p[(size_t)g * len] = w[(size_t)g * 16];
+    }
+}
+
+hipError_t kv8_weights(const Kv8Layer* layers, int n_heads, const RepackUnits& u, float* buf, bool in, hipStream_t s) {
+    if (u.n_units <= 0 || u.max_pages <= 0) return hipSuccess;
+    if (n_heads <= 0 || u.n_units > 65535) return hipErrorInvalidValue;
+    kv8_weights_kernel<<<dim3((u.max_pages + 15) / 16, u.n_units, n_heads < 64 ? n_heads : 64), 256, 0, s>>>(layers, n_heads, u, buf, in);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- eviction
+// Order of the weights as unsigned numbers: larger weight, larger number; -0 is 0, NaN is above everything.
+__device__ __forceinline__ uint32_t evict_key(float w) {
+    if (w != w) return 0xffffffffu;
+    const uint32_t b = __float_as_uint(w + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+// Which tokens stay.  A block per (head, layer, sequence).  The key of the last token that stays among the older ones is found digit
+// by digit (four histograms of 256), then one ordered pass lists the positions: all above that key, and of those
+// equal to it the first ones.
+constexpr int EV_T = 1024;
+__global__ __launch_bounds__(EV_T) void kv8_select_kernel(const Kv8Layer* __restrict__ layers, int n_heads, Kv8Evict e, int32_t* __restrict__ lists) {
+    __shared__ int hist[256], digit_s, left_s, eq_w[EV_T / 64], out_w[EV_T / 64];
+    const int g = blockIdx.x, layer = blockIdx.y, sq = blockIdx.z;
+    const int len = e.len[sq], keep = e.keep[sq];
+    if (len <= keep) return;
+    const int recent = e.recent < keep ? e.recent : keep;
+    const int n = len - recent, k = keep - recent;
+    const float* w = layers[layer].w;
+    const int32_t* pt = e.page_tables + (size_t)sq * e.pt_stride;
+    int32_t* list = lists + e.list_off[sq] + ((size_t)layer * n_heads + g) * keep;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int i = tid; i < recent; i += EV_T) list[k + i] = n + i;
+    if (k == 0) return;
+    auto key_at = [&](int t) { return evict_key(w[((size_t)pt[t >> 4] * n_heads + g) * 16 + (t & 15)]); };
+    uint32_t prefix = 0;
+    int left = k;                         // how many of those with the prefix stay
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int i = tid; i < 256; i += EV_T) hist[i] = 0;
+        __syncthreads();
+        for (int t = tid; t < n; t += EV_T) {
+            const uint32_t key = key_at(t);
+            if (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[key >> shift & 255], 1);
+        }
+        __syncthreads();
+        if (tid == 0) {
+            int d = 255, rest = left;
+            while (hist[d] < rest) rest -= hist[d--];
+            digit_s = d;
+            left_s = rest;
+        }
+        __syncthreads();
+        prefix |= (uint32_t)digit_s << shift;
+        left = left_s;
+        __syncthreads();
+    }
+    int n_eq = 0, n_out = 0;              // found in front of this stretch
+    for (int t0 = 0; t0 < n; t0 += EV_T) {
+        const int t = t0 + tid;
+        const uint32_t key = t < n ? key_at(t) : 0;
+        const bool eq = t < n && key == prefix, above = t < n && key > prefix;
+        const uint64_t eqm = __ballot(eq), lower = (1ull << lane) - 1;
+        if (lane == 0) eq_w[wave] = __popcll(eqm);
+        __syncthreads();
+        int eq_before = n_eq, eq_all = 0;
+        for (int i = 0; i < EV_T / 64; ++i) {
+            if (i < wave) eq_before += eq_w[i];
+            eq_all += eq_w[i];
+        }
+        const bool stays = above || (eq && eq_before + __popcll(eqm & lower) < left);
+        const uint64_t sm = __ballot(stays);
+        if (lane == 0) out_w[wave] = __popcll(sm);
+        __syncthreads();
+        int out_before = n_out, out_all = 0;
+        for (int i = 0; i < EV_T / 64; ++i) {
+            if (i < wave) out_before += out_w[i];
+            out_all += out_w[i];
+        }
+        if (stays) list[out_before + __popcll(sm & lower)] = t;
+        n_eq += eq_all;
+        n_out += out_all;
+        __syncthreads();
+    }
+}
+
+// Moves the kept tokens to the front, in place.  A block per (head, layer, sequence), a wave per new block of 16 tokens, 16 of them a
+// round.  Token s of the new cache comes from position list[s] >= s, so that a new block reads from pages at or behind its own: all
+// waves of a round load, then all store, and what later rounds read is still there.
+// In units of A / 127 the old values are q * A, exact in fp32 where A has the 16 bits of the model's type; those of the open
+// block are 127 * v.  The new block's magnitude in those units is W: A' = W / 127, q' = rint(value * 127 / W).  All in 32 bits,
+// for 32-bit models and blocks that were evicted before too, whose products are rounded.
+constexpr int EM_WAVES = 16;
+template <typename T, int D>
+__global__ __launch_bounds__(64 * EM_WAVES) void kv8_move_kernel(const Kv8Layer* __restrict__ layers, int n_heads, Kv8Evict e,
+                                                                 const int32_t* __restrict__ lists) {
+    const int g = blockIdx.x, layer = blockIdx.y, sq = blockIdx.z;
+    const int len = e.len[sq], keep = e.keep[sq];
+    if (len <= keep) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Kv8Layer kv = layers[layer];
+    const int32_t* pt = e.page_tables + (size_t)sq * e.pt_stride;
+    const int32_t* list = lists + e.list_off[sq] + ((size_t)layer * n_heads + g) * keep;
+    T* ko = (T*)kv.open + ((size_t)e.slot[sq] * 2 * n_heads + g) * 16 * D;
+    T* vo = ko + (size_t)n_heads * 16 * D;
+    const int full = len / 16;                               // full blocks of the old cache
+    const int blocks = (keep + 15) / 16;
+    constexpr int R = D / 64;                                // a lane has elements lane + 64 r of every token
+    for (int b0 = 0; b0 < blocks; b0 += EM_WAVES) {
+        const int blk = b0 + wave;
+        const int cnt = blk < blocks ? (keep - blk * 16 < 16 ? keep - blk * 16 : 16) : 0;
+        float xk[16][R], xv[16][R], w = 0.f;
+        float mk = 0.f, mv = 0.f;
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) xk[t][r] = xv[t][r] = 0.f;
+            if (t < cnt) {
+                const int p = list[blk * 16 + t];
+                if (p >= full * 16) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        xk[t][r] = ldf(ko + (p & 15) * D + lane + 64 * r);
+                        xv[t][r] = ldf(vo + (p & 15) * D + lane + 64 * r);
+                    }
+                } else {
+                    const size_t page = (size_t)pt[p >> 4] * n_heads + g;
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        xk[t][r] = (float)kv.k[page * 16 * D + (p & 15) * D + lane + 64 * r];
+                        xv[t][r] = (float)kv.v[page * 16 * D + (size_t)(lane + 64 * r) * 16 + (p & 15)];
+                    }
+                }
+            }
+        }
+        // magnitudes of the blocks the tokens come from: lane t has those of token t (127 for the open one, where the value is itself)
+        float ak = 0.f, av = 0.f;
+        if (lane < cnt) {
+            const int p = list[blk * 16 + lane];
+            const size_t page = (size_t)pt[p >> 4] * n_heads + g;
+            ak = p >= full * 16 ? 127.f : kv.amax[page * 2];
+            av = p >= full * 16 ? 127.f : kv.amax[page * 2 + 1];
+            w = kv.w[page * 16 + (p & 15)];
+        }
+        // scaled where a product could pass the largest float
+        const bool open_mine = lane < cnt && ak == 127.f && av == 127.f;
+        float top_k = open_mine ? 0.f : ak, top_v = open_mine ? 0.f : av;
+        const uint64_t opens = __ballot(open_mine);
+#pragma unroll
+        for (int t = 0; t < 16; ++t)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (opens >> t & 1) {
+                    top_k = fmaxf(top_k, fabsf(xk[t][r]));
+                    top_v = fmaxf(top_v, fabsf(xv[t][r]));
+                }
+        const float fk = kv8_fit(wave_max(top_k)), fv = kv8_fit(wave_max(top_v));
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+            const float sk = __shfl(ak, t, 64) * fk, sv = __shfl(av, t, 64) * fv;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                xk[t][r] *= sk;
+                xv[t][r] *= sv;
+                mk = fmaxf(mk, kv8_mag(xk[t][r]));
+                mv = fmaxf(mv, kv8_mag(xv[t][r]));
+            }
+        }
+        mk = wave_max(mk);
+        mv = wave_max(mv);
+        __syncthreads();                                     // the round has read what it moves
+        if (cnt > 0) {
+            const size_t page = (size_t)pt[blk] * n_heads + g;
+            if (lane < cnt) kv.w[page * 16 + lane] = w;
+            if (cnt == 16) {
+                if (lane == 0) {
+                    kv.amax[page * 2] = kv8_amax(mk) / 127.f / fk;
+                    kv.amax[page * 2 + 1] = kv8_amax(mv) / 127.f / fv;
+                }
+                const float gk = kv8_fit(mk), gv = kv8_fit(mv);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    vec16 o;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        int q[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            kv.k[page * 16 * D + (4 * i + j) * D + lane + 64 * r] = (int8_t)kv8_round<bf16_t>(xk[4 * i + j][r] * gk, mk * gk);
+                            q[j] = kv8_round<bf16_t>(xv[4 * i + j][r] * gv, mv * gv);
+                        }
+                        o.w[i] = kv8_pack4(q);
+                    }
+                    *reinterpret_cast<vec16*>(kv.v + page * 16 * D + (size_t)(lane + 64 * r) * 16) = o;
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < 16; ++t)
+                    if (t < cnt)
+#pragma unroll
+                        for (int r = 0; r < R; ++r) {
+                            stf(ko + t * D + lane + 64 * r, xk[t][r] / fk / 127.f);
+                            stf(vo + t * D + lane + 64 * r, xv[t][r] / fv / 127.f);
+                        }
+            }
+        }
+    }
+}
+
+template <typename T, int D>
+static void launch_move(const Kv8Layer* layers, int n_heads, const Kv8Evict& e, const int32_t* lists, dim3 grid, hipStream_t s) {
+    kv8_move_kernel<T, D><<<grid, 64 * EM_WAVES, 0, s>>>(layers, n_heads, e, lists);
+}
+
+hipError_t kv8_evict(int dt, const Kv8Layer* layers, int n_heads, int d, const Kv8Evict& e, int32_t* lists, hipStream_t s) {
+    if (e.n_seqs <= 0) return hipSuccess;
+    if ((d != 64 && d != 128) || n_heads <= 0 || e.n_layers <= 0 || e.n_layers > 65535 || e.n_seqs > 65535 || !lists || e.recent < 0)
+        return hipErrorInvalidValue;
+    const dim3 grid(n_heads, e.n_layers, e.n_seqs);
+    kv8_select_kernel<<<grid, EV_T, 0, s>>>(layers, n_heads, e, lists);
+    SS_TYPED(dt, d, launch_move, (layers, n_heads, e, lists, grid, s));
+    return hipGetLastError();
+}
+
+}  // namespace SS_NS

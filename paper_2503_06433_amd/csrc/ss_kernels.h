@@ -104,6 +104,53 @@ struct RepackUnits {
     const int32_t* pages;        // concatenated page lists
     int n_units;
     int max_pages;               // most pages of any unit
+    const int32_t* unit_slot;    // open block of the unit's sequence (8-bit caches only)
+};
+
+// One layer of a cache in 8 bits.  A block is 16 tokens of one kv head, K and V apart.  A full block with the largest magnitude A
+// holds the whole numbers q = v * 127 / A, to nearest even, and stands for q * (A / 127); a block with a value that is not
+// finite stands for NaN throughout.  The last block of a sequence is kept in the model's type as well, in the sequence's
+// open block, and is read from there until it is full.
+//   K page: [head][16][d]    V page: [head][d][16], tokens in order    page p starts at p * n_heads * 16 * d
+struct Kv8Layer {
+    int8_t* k;
+    int8_t* v;
+    float* amax;         // [page][head][K | V]
+    void* open;          // [slot][K | V][head][16][d], model dtype
+    float* w;            // [page][head][16] accumulated attention weights, or null
+};
+
+// Batch over 8-bit caches (device arrays).  Positions are counted in cached tokens; `pos` is what the rotary embedding sees.
+struct Kv8Batch {
+    const int32_t* page_tables;
+    int pt_stride;
+    const int32_t* cu_q;         // [n_seqs + 1]
+    const int32_t* before;       // [n_seqs] cached position of a sequence's first token of the batch
+    const int32_t* end;          // [n_seqs] cached tokens of the layer once the batch's are in: blocks below end / 16 are full
+    const int32_t* slot;         // [n_seqs]
+    const int32_t* pos;          // [n_seqs]
+    const int32_t* tok_off;      // [n_seqs] tokens that the sequences in front see (weights only)
+    int n_seqs, T, max_q_len, max_seen;
+    int64_t seen;                // tokens that all sequences see
+    const int32_t* unit_seq;     // page units of the new tokens, as in BatchMeta
+    const int32_t* unit_tok0;
+    const int32_t* unit_pos0;
+    const int32_t* unit_cnt;
+    int n_units;
+    const int32_t* pf_items;
+    int pf_stride, pf_blocks;
+    DecodeWork wk;               // pages include the open block's
+};
+
+// Sequences of an eviction (device arrays).
+struct Kv8Evict {
+    const int32_t* page_tables;
+    int pt_stride;
+    const int32_t* len;          // cached tokens
+    const int32_t* keep;
+    const int32_t* slot;
+    const int64_t* list_off;     // [n_seqs] where a sequence's lists [layer][head][keep] start
+    int n_seqs, n_layers, recent, max_len;
 };
 
 }  // namespace ssk
@@ -219,7 +266,32 @@ hipError_t argmax_rows(const float* logits, int n, int V, int32_t* out, hipStrea
 // dst[i] = src[i] for i < n (elements of the model dtype); used for gains.
 hipError_t copy_elems(int dt, const void* src, void* dst, int64_t n, hipStream_t s);
 
+// ---- caches in 8 bits (Kv8Layer)
+// Rotates q and k in place inside qkv [T, (n_q + 2 n_kv) d].
+hipError_t kv8_rope(int dt, void* qkv, int n_q, int n_kv, int d, const float* rope_table, const Kv8Batch& b, hipStream_t s);
 
+// The batch's new tokens into the cache.  k, v: rows of n_heads * d elements, `k_stride` / `v_stride` elements apart.
+hipError_t kv8_write(int dt, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int n_heads, int d, const Kv8Batch& b,
+                     const Kv8Layer& kv, hipStream_t s);
+
+// Whole sequences from and into heads-major staging in the model's type; `layers` is a device array.
+hipError_t kv8_gather(int dt, const Kv8Layer* layers, int n_heads, int d, const RepackUnits& u, void* staging, hipStream_t s);
+hipError_t kv8_scatter(int dt, const Kv8Layer* layers, int n_heads, int d, const RepackUnits& u, const void* staging, hipStream_t s);
+
+// Accumulated weights of whole sequences, buf [unit][head][token]; unit_off counts those.
+hipError_t kv8_weights(const Kv8Layer* layers, int n_heads, const RepackUnits& u, float* buf, bool in, hipStream_t s);
+
+// Cuts every sequence to keep[] tokens; `lists`: workspace of int32, see Kv8Evict::list_off.
+hipError_t kv8_evict(int dt, const Kv8Layer* layers, int n_heads, int d, const Kv8Evict& e, int32_t* lists, hipStream_t s);
+
+// Causal attention of the batch's queries over the cache (which has their tokens).  q: rows `q_stride` elements apart, out [T, n_q d].
+hipError_t attn8_prefill(int dt, const void* q, int64_t q_stride, void* out, int n_q, int n_kv, int d, const Kv8Batch& b,
+                         const Kv8Layer& kv, bool force_generic, hipStream_t s);
+
+// One query per sequence.  With kv.w the weights of all query heads are added to it.  scratch: attn8_decode_scratch_floats.
+size_t attn8_decode_scratch_floats(const Kv8Batch& b, int n_q, int d, bool weights);
+hipError_t attn8_decode(int dt, const void* q, int64_t q_stride, void* out, int n_q, int n_kv, int d, const Kv8Batch& b,
+                        const Kv8Layer& kv, float* scratch, bool force_generic, hipStream_t s);
 
 }  // namespace SS_DECL_NS
 #undef SS_DECL_NS

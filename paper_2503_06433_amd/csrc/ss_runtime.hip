@@ -65,6 +65,11 @@ struct SeqState {
     std::vector<int32_t> pages;
     int32_t len = 0;
     uint64_t seen = 0;         // batch that listed the sequence last (ss_ctx::batches)
+    // caches in 8 bits
+    int32_t slot = -1;                   // of the open block
+    std::vector<int32_t> layer_len;      // cached tokens of every layer; len is the largest of them
+    int32_t evicted = 0;                 // positions that are no longer cached: cached position = position - evicted
+    int32_t floor = 0;                   // cached position that batches may not go back behind
 };
 
 struct Shard {
@@ -80,6 +85,13 @@ struct Shard {
     uint64_t version = 0;     // bumped on every page-table change
     hipEvent_t w_ready = nullptr;   // recorded on the weight stream behind the shard's last (re)load
     bool w_pending = false;         // ... which layer calls still have to wait for
+    // cache in 8 bits: k_pool / v_pool hold its pages
+    bool kv8 = false, kv8_weights = false;
+    int32_t kv8_slots = 0;
+    std::vector<ssk::Kv8Layer> kv8_layers;
+    ssk::Kv8Layer* d_kv8_layers = nullptr;
+    std::vector<void*> kv8_mem;                   // everything allocated for it
+    std::priority_queue<int32_t, std::vector<int32_t>, std::greater<int32_t>> free_slots;
 };
 
 struct DescKey {
@@ -108,6 +120,24 @@ struct MetaSlot {
     ssk::DecodeWork wk{};
 };
 
+// The same for batches over caches in 8 bits.
+struct Meta8Slot {
+    uint8_t* host = nullptr;
+    uint8_t* dev = nullptr;
+    size_t cap = 0;
+    hipEvent_t done = nullptr;
+    bool in_flight = false;
+    ssk::UploadJob job;
+    bool pending = false;
+    // cache key
+    Shard* shard = nullptr;
+    uint64_t version = 0;
+    bool decode = false, write = false;
+    std::vector<int64_t> seq_ids;
+    std::vector<int32_t> q_lens, before, end, pos;
+    ssk::Kv8Batch b{};
+};
+
 // Metadata images of the device-side export / import: the halves of the swap-out lane's metadata region, in turn.  The calls
 // and that lane keep out of each other's way: a call starts when the lanes are idle, a swap-out job waits for `done`.
 struct XferSlot {
@@ -121,6 +151,7 @@ struct SeqJob {
     int32_t len;
     std::vector<int32_t> pages;
     size_t tier_off;   // bytes
+    int32_t slot = 0;  // of the open block (caches in 8 bits)
 };
 
 struct Job {
@@ -343,6 +374,8 @@ struct ss_ctx {
     DevBuf ws_h, ws_qkv, ws_attn, ws_act, ws_x1, ws_scratch, ws_splitk, ws_chain[2];
     MetaSlot meta[4];
     int meta_next = 0;
+    Meta8Slot meta8[4];
+    int meta8_next = 0;
     uint64_t batches = 0;      // metadata built so far
     XferSlot xfer[2];
     int xfer_next = 0;
@@ -484,8 +517,45 @@ int get_shard(ss_ctx* c, const ss_shard_desc* d, Shard** out) {
 
 size_t page_bytes(ss_ctx* c, Shard* s) { return (size_t)s->nkv_l * c->m.page_size * c->m.head_dim * c->es; }
 
+// Pages in 8 bits, their magnitudes, open blocks and, where they are kept, attention weights.  All or nothing.
+int ensure_pools8(ss_ctx* c, Shard* s) {
+    const size_t pages = (size_t)c->rt.gpu_kv_pages, heads = s->nkv_l, block = (size_t)16 * c->m.head_dim;
+    std::vector<ssk::Kv8Layer> layers(s->n_layers_l);
+    std::vector<void*> mem;
+    auto get = [&](void** p, size_t bytes) -> hipError_t {
+        hipError_t e = hipMalloc(p, bytes);
+        if (e != hipSuccess) return e;
+        mem.push_back(*p);
+        return hipMemset(*p, 0, bytes);
+    };
+    hipError_t e = hipSuccess;
+    for (ssk::Kv8Layer& l : layers) {
+        l = {};
+        if (e == hipSuccess) e = get((void**)&l.k, pages * heads * block);
+        if (e == hipSuccess) e = get((void**)&l.v, pages * heads * block);
+        if (e == hipSuccess) e = get((void**)&l.amax, pages * heads * 2 * sizeof(float));
+        if (e == hipSuccess) e = get(&l.open, (size_t)s->kv8_slots * 2 * heads * block * c->es);
+        if (e == hipSuccess && s->kv8_weights) e = get((void**)&l.w, pages * heads * 16 * sizeof(float));
+    }
+    ssk::Kv8Layer* d = nullptr;
+    if (e == hipSuccess) e = get((void**)&d, sizeof(ssk::Kv8Layer) * layers.size());
+    if (e == hipSuccess) e = hipMemcpy(d, layers.data(), sizeof(ssk::Kv8Layer) * layers.size(), hipMemcpyHostToDevice);
+    if (e != hipSuccess) {
+        for (void* p : mem) (void)hipFree(p);
+        return fail(c, e == hipErrorOutOfMemory ? SS_ENOMEM : SS_EHIP, "cache in 8 bits: %s", hipGetErrorString(e));
+    }
+    s->kv8_layers = std::move(layers);
+    s->d_kv8_layers = d;
+    s->kv8_mem = std::move(mem);
+    for (int32_t i = 0; i < s->kv8_slots; ++i) s->free_slots.push(i);
+    for (int64_t p = 0; p < c->rt.gpu_kv_pages; ++p) s->free_pages.push((int32_t)p);
+    s->pools_ready = true;
+    return SS_OK;
+}
+
 int ensure_pools(ss_ctx* c, Shard* s) {
     if (s->pools_ready) return SS_OK;
+    if (s->kv8) return ensure_pools8(c, s);
     const size_t bytes = page_bytes(c, s) * (size_t)c->rt.gpu_kv_pages;
     s->k_pool.assign(s->n_layers_l, nullptr);
     s->v_pool.assign(s->n_layers_l, nullptr);
@@ -516,8 +586,15 @@ int ensure_pages(ss_ctx* c, Shard* s, int64_t seq, int32_t length) {
         if (need > have && need - have > s->free_pages.size())
             return fail(c, SS_ENOMEM, "page pool exhausted: sequence %lld needs %zu more pages, %zu free",
                         (long long)seq, need - have, s->free_pages.size());
+        if (s->kv8 && it == s->seqs.end() && s->free_slots.empty())
+            return fail(c, SS_ENOMEM, "sequence %lld: all %d sequences of the cache in 8 bits are taken", (long long)seq, s->kv8_slots);
     }
     SeqState& st = s->seqs[seq];
+    if (s->kv8 && st.slot < 0) {
+        st.slot = s->free_slots.top();
+        s->free_slots.pop();
+        st.layer_len.assign(s->n_layers_l, 0);
+    }
     if (need > st.pages.size()) {
         while (st.pages.size() < need) {
             st.pages.push_back(s->free_pages.top());
@@ -538,7 +615,32 @@ int check_new_seqs_fit(ss_ctx* c, Shard* s, const int32_t* lens, int n) {
     if (need > s->free_pages.size())
         return fail(c, SS_ENOMEM, "page pool exhausted: the %d sequences need %zu pages, %zu free", n, need,
                     s->free_pages.size());
+    if (s->kv8 && (size_t)n > s->free_slots.size())
+        return fail(c, SS_ENOMEM, "%d sequences, %zu of %d left in the cache in 8 bits", n, s->free_slots.size(), s->kv8_slots);
     return SS_OK;
+}
+
+// A whole sequence has come on board: every layer has its tokens.
+void kv8_arrived(Shard* s, SeqState& st) {
+    if (s->kv8) std::fill(st.layer_len.begin(), st.layer_len.end(), st.len);
+}
+
+// What leaves or is cut as a whole has to be there in every layer.
+int kv8_whole(ss_ctx* c, Shard* s, int64_t seq, const SeqState& st) {
+    for (int l = 0; s->kv8 && l < s->n_layers_l; ++l)
+        if (st.layer_len[l] != st.len)
+            return fail(c, SS_EINVAL, "sequence %lld: layer %d holds %d tokens, another %d", (long long)seq, s->desc.layer_begin + l,
+                        st.layer_len[l], st.len);
+    return SS_OK;
+}
+
+// Pages <-> heads-major staging, whichever way the pages are kept.
+hipError_t repack(ss_ctx* c, Shard* s, bool into_pages, const ssk::RepackUnits& ru, void* staging, hipStream_t st) {
+    if (s->kv8)
+        return into_pages ? SSK_CALL(c, kv8_scatter, s->d_kv8_layers, s->nkv_l, c->m.head_dim, ru, staging, st)
+                          : SSK_CALL(c, kv8_gather, s->d_kv8_layers, s->nkv_l, c->m.head_dim, ru, staging, st);
+    return into_pages ? SSK_CALL(c, kv_scatter, s->d_k_pools, s->d_v_pools, s->nkv_l, c->m.head_dim, c->m.page_size, ru, staging, st)
+                      : SSK_CALL(c, kv_gather, s->d_k_pools, s->d_v_pools, s->nkv_l, c->m.head_dim, c->m.page_size, ru, staging, st);
 }
 
 ssk::KvLayer kv_layer(ss_ctx* c, Shard* s, int ll) {
@@ -566,6 +668,70 @@ static int decode_item_pages(int64_t total_pages, int n_kv_local) {
     int64_t n = total_pages * n_kv_local / 2048;
     n = std::max<int64_t>(16, std::min<int64_t>(64, n));
     return (int)(n & ~1);
+}
+
+// Prefill attention work lists.  An item is (sequence, q head, block of 256 queries); its cost is the
+// number of 64-token tiles it visits plus a fixed part.  The blocks of the kernel (one per compute unit)
+// are dealt to the 8 XCDs round-robin by their index, so the items of one (sequence, kv head) -- which
+// read the same K and V pages -- all go to blocks of one residue modulo 8 and find those pages in one
+// L2.  Within a residue the items are taken sequence by sequence (longest first), kv head by kv head, last
+// query block first, and each goes to the block with the least work so far: the items of one (sequence,
+// kv head) then start at about the same time on different blocks and share the pages while they are in
+// the L2 (taking all items heaviest first balances 2 % better and reads twice as much from beyond L2).
+void prefill_items(ss_ctx* c, Shard* s, int n, const int32_t* q_lens, const int32_t* kv_before, std::vector<int32_t>* items,
+                   int* stride_out, int* blocks_out) {
+    struct PfItem { int32_t sq, a, qb, cost, len; };
+    const int G = s->nq_l / s->nkv_l;
+    const int per_x = std::max(1, c->n_cus / 8);
+    std::vector<std::vector<PfItem>> by_x(8);
+    for (int i = 0; i < n; ++i) {
+        const int nqb_i = (q_lens[i] + 255) / 256;
+        for (int g = 0; g < s->nkv_l; ++g) {
+            const int x = (int)(((int64_t)i * s->nkv_l + g) % 8);
+            for (int jg = 0; jg < G; ++jg)
+                for (int qb = 0; qb < nqb_i; ++qb) {
+                    const int last = kv_before[i] + std::min(qb * 256 + 255, q_lens[i] - 1);
+                    by_x[x].push_back({i, g * G + jg, qb, last / 64 + 1 + 2, kv_before[i] + q_lens[i]});
+                }
+        }
+    }
+    std::vector<std::vector<PfItem>> lists((size_t)8 * per_x);
+    for (int x = 0; x < 8; ++x) {
+        std::stable_sort(by_x[x].begin(), by_x[x].end(), [G](const PfItem& p, const PfItem& q) {
+            if (p.len != q.len) return p.len > q.len;
+            if (p.sq != q.sq) return p.sq < q.sq;
+            if (p.a / G != q.a / G) return p.a / G < q.a / G;
+            if (p.qb != q.qb) return p.qb > q.qb;
+            return p.a < q.a;
+        });
+        std::priority_queue<std::pair<int64_t, int>, std::vector<std::pair<int64_t, int>>, std::greater<std::pair<int64_t, int>>> load;
+        for (int k = 0; k < per_x; ++k) load.push({0, k});
+        for (const PfItem& it : by_x[x]) {
+            auto top = load.top();
+            load.pop();
+            lists[(size_t)top.second * 8 + x].push_back(it);
+            load.push({top.first + it.cost, top.second});
+        }
+    }
+    const int pf_blocks = *blocks_out = 8 * per_x;
+    size_t longest = 0;
+    for (const auto& l : lists) longest = std::max(longest, l.size());
+    const int pf_stride = *stride_out = (int)longest + 1;
+    // one 32-byte record per item, everything the block needs to start on it: sequence (-1 ends the
+    // list), q head, first query of the block, first token of the sequence in the batch, its number of
+    // new tokens, its number of cached tokens
+    std::vector<int32_t>& pf_items = *items;
+    pf_items.assign((size_t)pf_blocks * pf_stride * 8, -1);
+    int t0 = 0;
+    std::vector<int> q_begin(n);
+    for (int i = 0; i < n; ++i) { q_begin[i] = t0; t0 += q_lens[i]; }
+    for (int blk = 0; blk < pf_blocks; ++blk)
+        for (size_t j = 0; j < lists[blk].size(); ++j) {
+            int32_t* r = &pf_items[((size_t)blk * pf_stride + j) * 8];
+            const PfItem& it = lists[blk][j];
+            r[0] = it.sq; r[1] = it.a; r[2] = it.qb * 256; r[3] = q_begin[it.sq]; r[4] = q_lens[it.sq];
+            r[5] = kv_before[it.sq]; r[6] = 0; r[7] = 0;
+        }
 }
 
 // Builds (or reuses) the metadata of a batch.  Returns the slot, whose upload may still have to be made (`pending`).
@@ -695,69 +861,9 @@ int prepare_batch(ss_ctx* c, Shard* s, const ss_batch* b, bool decode, MetaSlot*
     }
     const size_t n_units = unit_seq.size();
     const size_t n_items = item_seq.size();
-    // Prefill attention work lists.  An item is (sequence, q head, block of 256 queries); its cost is the
-    // number of 64-token tiles it visits plus a fixed part.  The blocks of the kernel (one per compute unit)
-    // are dealt to the 8 XCDs round-robin by their index, so the items of one (sequence, kv head) -- which
-    // read the same K and V pages -- all go to blocks of one residue modulo 8 and find those pages in one
-    // L2.  Within a residue the items are taken sequence by sequence (longest first), kv head by kv head, last
-    // query block first, and each goes to the block with the least work so far: the items of one (sequence,
-    // kv head) then start at about the same time on different blocks and share the pages while they are in
-    // the L2 (taking all items heaviest first balances 2 % better and reads twice as much from beyond L2).
     std::vector<int32_t> pf_items;
     int pf_stride = 0, pf_blocks = 0;
-    if (!decode && max_q > 64) {
-        struct PfItem { int32_t sq, a, qb, cost, len; };
-        const int G = s->nq_l / s->nkv_l;
-        const int per_x = std::max(1, c->n_cus / 8);
-        std::vector<std::vector<PfItem>> by_x(8);
-        for (int i = 0; i < n; ++i) {
-            const int nqb_i = (b->q_lens[i] + 255) / 256;
-            for (int g = 0; g < s->nkv_l; ++g) {
-                const int x = (int)(((int64_t)i * s->nkv_l + g) % 8);
-                for (int jg = 0; jg < G; ++jg)
-                    for (int qb = 0; qb < nqb_i; ++qb) {
-                        const int last = b->kv_lens_before[i] + std::min(qb * 256 + 255, b->q_lens[i] - 1);
-                        by_x[x].push_back({i, g * G + jg, qb, last / 64 + 1 + 2, b->kv_lens_before[i] + b->q_lens[i]});
-                    }
-            }
-        }
-        std::vector<std::vector<PfItem>> lists((size_t)8 * per_x);
-        for (int x = 0; x < 8; ++x) {
-            std::stable_sort(by_x[x].begin(), by_x[x].end(), [G](const PfItem& p, const PfItem& q) {
-                if (p.len != q.len) return p.len > q.len;
-                if (p.sq != q.sq) return p.sq < q.sq;
-                if (p.a / G != q.a / G) return p.a / G < q.a / G;
-                if (p.qb != q.qb) return p.qb > q.qb;
-                return p.a < q.a;
-            });
-            std::priority_queue<std::pair<int64_t, int>, std::vector<std::pair<int64_t, int>>, std::greater<std::pair<int64_t, int>>> load;
-            for (int k = 0; k < per_x; ++k) load.push({0, k});
-            for (const PfItem& it : by_x[x]) {
-                auto top = load.top();
-                load.pop();
-                lists[(size_t)top.second * 8 + x].push_back(it);
-                load.push({top.first + it.cost, top.second});
-            }
-        }
-        pf_blocks = 8 * per_x;
-        size_t longest = 0;
-        for (const auto& l : lists) longest = std::max(longest, l.size());
-        pf_stride = (int)longest + 1;
-        // one 32-byte record per item, everything the block needs to start on it: sequence (-1 ends the
-        // list), q head, first query of the block, first token of the sequence in the batch, its number of
-        // new tokens, its number of cached tokens
-        pf_items.assign((size_t)pf_blocks * pf_stride * 8, -1);
-        int t0 = 0;
-        std::vector<int> q_begin(n);
-        for (int i = 0; i < n; ++i) { q_begin[i] = t0; t0 += b->q_lens[i]; }
-        for (int blk = 0; blk < pf_blocks; ++blk)
-            for (size_t j = 0; j < lists[blk].size(); ++j) {
-                int32_t* r = &pf_items[((size_t)blk * pf_stride + j) * 8];
-                const PfItem& it = lists[blk][j];
-                r[0] = it.sq; r[1] = it.a; r[2] = it.qb * 256; r[3] = q_begin[it.sq]; r[4] = b->q_lens[it.sq];
-                r[5] = b->kv_lens_before[it.sq]; r[6] = 0; r[7] = 0;
-            }
-    }
+    if (!decode && max_q > 64) prefill_items(c, s, n, b->q_lens, b->kv_lens_before, &pf_items, &pf_stride, &pf_blocks);
     // launch order: longest items first, so that the last waves of the grid are the short ones
     std::vector<int32_t> item_order(n_items);
     for (size_t i = 0; i < n_items; ++i) item_order[i] = (int32_t)i;
@@ -950,6 +1056,272 @@ int run_attn_phase(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, 
     return mark_meta_used(c, ms, st);
 }
 
+// ------------------------------------------------------------------ caches in 8 bits
+// Pages per work item of a decode step over a cache in 8 bits, a multiple of the four that the kernel takes at a time.
+static int decode8_item_pages(int64_t total_pages, int n_kv_local) {
+    const int64_t n = std::max<int64_t>(16, std::min<int64_t>(64, total_pages * n_kv_local / 2048));
+    return (int)(n & ~3);
+}
+
+int refuse_capture(ss_ctx* c, hipStream_t st) {
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    HIP_TRY(c, hipStreamIsCapturing(st, &cap));
+    if (cap != hipStreamCaptureStatusNone) return fail(c, SS_EHIP, "cache in 8 bits: the stream is capturing");
+    return SS_OK;
+}
+
+void wait_seqs_idle(ss_ctx* c, const Shard* sh, const int64_t* ids, int n);
+
+// A slot whose images hold `total` bytes and whose last user is through.
+int meta8_slot(ss_ctx* c, size_t total, Meta8Slot** out) {
+    Meta8Slot& ms = c->meta8[c->meta8_next];
+    c->meta8_next = (c->meta8_next + 1) % 4;
+    if (ms.in_flight) {
+        HIP_TRY(c, hipEventSynchronize(ms.done));
+        ms.in_flight = false;
+    }
+    ms.shard = nullptr;
+    if (total > ms.cap) {
+        ms.cap = 0;
+        if (ms.host) { HIP_TRY(c, hipHostFree(ms.host)); ms.host = nullptr; }
+        if (ms.dev) { HIP_TRY(c, hipFree(ms.dev)); ms.dev = nullptr; }
+        const size_t cap = total + total / 4 + 4096;
+        HIP_TRY(c, hipHostMalloc((void**)&ms.host, cap, hipHostMallocDefault));
+        HIP_TRY(c, hipMalloc((void**)&ms.dev, cap));
+        ms.cap = cap;
+    }
+    void* mapped = nullptr;
+    HIP_TRY(c, hipHostGetDevicePointer(&mapped, ms.host, 0));
+    ms.job = {mapped, ms.dev, (int64_t)((total + 15) / 16)};
+    ms.pending = true;
+    *out = &ms;
+    return SS_OK;
+}
+
+int mark_meta8_used(ss_ctx* c, Meta8Slot* ms, hipStream_t stream) {
+    if (!ms->done) HIP_TRY(c, hipEventCreateWithFlags(&ms->done, hipEventDisableTiming));
+    HIP_TRY(c, hipEventRecord(ms->done, stream));
+    ms->in_flight = true;
+    return SS_OK;
+}
+
+// Arrays of one image, each at a multiple of 64 bytes.
+struct Image {
+    size_t total = 0;
+    std::vector<std::pair<size_t, std::pair<const void*, size_t>>> parts;
+    template <class T> size_t add(const std::vector<T>& v) {
+        const size_t at = total;
+        if (!v.empty()) parts.push_back({at, {v.data(), v.size() * sizeof(T)}});
+        total += (v.size() * sizeof(T) + 63) & ~(size_t)63;
+        return at;
+    }
+    void write(uint8_t* to) const {
+        for (const auto& p : parts) memcpy(to + p.first, p.second.first, p.second.second);
+    }
+};
+
+// Checks a batch over a cache in 8 bits, takes the pages of what it brings, builds (or finds) its metadata.  Nothing is changed unless
+// everything fits.
+int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool write, Meta8Slot** out) {
+    const int n = b->n_seqs, ps = 16;
+    std::vector<int32_t> before(n), end(n), slot(n), pos(n);
+    int64_t T = 0, seen = 0;
+    int max_q = 0, max_seen = 0;
+    size_t more = 0, fresh = 0;
+    ++c->batches;
+    for (int i = 0; i < n; ++i) {
+        const int64_t id = b->seq_ids[i];
+        const int ql = b->q_lens[i], at = b->kv_lens_before[i];
+        if (ql <= 0 || at < 0) return fail(c, SS_EINVAL, "sequence %d: q_len=%d kv_len_before=%d", i, ql, at);
+        if (decode && ql != 1) return fail(c, SS_EINVAL, "decode needs q_len == 1 (sequence %d has %d)", i, ql);
+        if ((int64_t)at + ql > c->rt.max_seq_len)
+            return fail(c, SS_EINVAL, "sequence %d reaches length %lld > max_seq_len %d", i, (long long)at + ql, c->rt.max_seq_len);
+        auto it = s->seqs.find(id);
+        SeqState* st = it == s->seqs.end() ? nullptr : &it->second;
+        const int have = st ? st->layer_len[ll] : 0, gone = st ? st->evicted : 0, floor = st ? st->floor : 0;
+        const int cached = at - gone;                       // the position among the cached tokens
+        if (st && st->seen == c->batches) return fail(c, SS_EINVAL, "sequence %lld is listed twice", (long long)id);
+        if (st) st->seen = c->batches;
+        if (write) {
+            if (at > 0 && (!st || cached > have))
+                return fail(c, SS_ENOENT, "sequence %lld has no %d cached tokens in this shard", (long long)id, at);
+            if (st && cached < floor)
+                return fail(c, SS_EINVAL, "sequence %lld: position %d lies before its eviction", (long long)id, at);
+            if (cached % ps && cached / ps != (have - 1) / ps)
+                return fail(c, SS_EINVAL, "sequence %lld: a cache of %d tokens in 8 bits cannot be cut back to %d, only to a multiple of %d or "
+                                          "inside its last block", (long long)id, have, cached, ps);
+            end[i] = cached + ql;
+        } else {
+            if (!st || cached + ql > have)
+                return fail(c, SS_ENOENT, "sequence %lld has no %d cached tokens in this shard", (long long)id, at + ql);
+            if (cached < floor - 1 || cached < 0)
+                return fail(c, SS_EINVAL, "sequence %lld: position %d lies before its eviction", (long long)id, at);
+            end[i] = have;
+        }
+        before[i] = cached;
+        pos[i] = at;
+        const size_t need = (size_t)(end[i] + ps - 1) / ps, pages = st ? st->pages.size() : 0;
+        if (need > pages) more += need - pages;
+        fresh += !st;
+        T += ql;
+        seen += cached + ql;
+        max_q = std::max(max_q, ql);
+        max_seen = std::max(max_seen, cached + ql);
+    }
+    for (int i = 0; fresh > 1 && i < n; ++i)                // sequences that nobody knows yet are compared among themselves
+        if (!s->seqs.count(b->seq_ids[i]))
+            for (int j = 0; j < i; ++j)
+                if (b->seq_ids[j] == b->seq_ids[i]) return fail(c, SS_EINVAL, "sequence %lld is listed twice", (long long)b->seq_ids[i]);
+    if (T > (1 << 30)) return fail(c, SS_EINVAL, "batch too large");
+    if (decode && s->kv8_weights && seen > INT32_MAX) return fail(c, SS_EINVAL, "batch too large: it sees %lld tokens", (long long)seen);
+    if (more > s->free_pages.size())
+        return fail(c, SS_ENOMEM, "page pool exhausted: the batch needs %zu more pages, %zu free", more, s->free_pages.size());
+    if (fresh > s->free_slots.size())
+        return fail(c, SS_ENOMEM, "%zu new sequences, %zu of %d left in the cache in 8 bits", fresh, s->free_slots.size(), s->kv8_slots);
+    if (write) {
+        // a swap-out that has not run yet reads the open blocks
+        wait_seqs_idle(c, s, b->seq_ids, n);
+        for (int i = 0; i < n; ++i) {
+            int rc = ensure_pages(c, s, b->seq_ids[i], end[i]);
+            if (rc) return rc;
+            SeqState& st = s->seqs[b->seq_ids[i]];
+            st.layer_len[ll] = end[i];
+            st.len = *std::max_element(st.layer_len.begin(), st.layer_len.end());
+        }
+    }
+    for (auto& ms : c->meta8)
+        if (ms.shard == s && ms.version == s->version && ms.decode == decode && ms.write == write && (int)ms.seq_ids.size() == n &&
+            std::equal(ms.seq_ids.begin(), ms.seq_ids.end(), b->seq_ids) && std::equal(ms.q_lens.begin(), ms.q_lens.end(), b->q_lens) &&
+            ms.before == before && ms.end == end && ms.pos == pos) {
+            *out = &ms;
+            return SS_OK;
+        }
+    // ---- build
+    int pt_stride = 1;
+    std::vector<const SeqState*> sts(n);
+    std::vector<int32_t> cu(n + 1), tok_off(n);
+    int32_t t = 0, o = 0;
+    for (int i = 0; i < n; ++i) {
+        sts[i] = &s->seqs[b->seq_ids[i]];
+        slot[i] = sts[i]->slot;
+        pt_stride = std::max<int>(pt_stride, (int)sts[i]->pages.size());
+        cu[i] = t;
+        t += b->q_lens[i];
+        if (decode && s->kv8_weights) { tok_off[i] = o; o += before[i] + 1; }
+    }
+    cu[n] = t;
+    std::vector<int32_t> pt((size_t)n * pt_stride, 0);
+    for (int i = 0; i < n; ++i) std::copy(sts[i]->pages.begin(), sts[i]->pages.end(), pt.begin() + (size_t)i * pt_stride);
+    std::vector<int32_t> unit_seq, unit_tok0, unit_pos0, unit_cnt;
+    for (int i = 0; write && i < n; ++i)
+        for (int pg = before[i] / ps; pg * ps < end[i]; ++pg) {
+            const int p0 = std::max(before[i], pg * ps), p1 = std::min(end[i], pg * ps + ps);
+            unit_seq.push_back(i);
+            unit_tok0.push_back(cu[i] + (p0 - before[i]));
+            unit_pos0.push_back(p0);
+            unit_cnt.push_back(p1 - p0);
+        }
+    // near-equal items of a sequence, interleaved: item j takes the pages j, j + cnt, ...
+    std::vector<int32_t> item_seq, item_page0, item_np, seq_item0, item_order;
+    int max_items = 0;
+    if (decode) {
+        int64_t total_pages = 0;
+        for (int i = 0; i < n; ++i) total_pages += before[i] / ps + 1;
+        const int ipp = decode8_item_pages(total_pages, s->nkv_l);
+        for (int i = 0; i < n; ++i) {
+            seq_item0.push_back((int32_t)item_seq.size());
+            const int used = before[i] / ps + 1, cnt = std::min((used + ipp - 1) / ipp, 65535);
+            for (int j = 0; j < cnt; ++j) {
+                item_seq.push_back(i);
+                item_page0.push_back(j);
+                item_np.push_back(((used - j + cnt - 1) / cnt) | (int)((unsigned)cnt << 16));
+            }
+            max_items = std::max(max_items, cnt);
+        }
+        seq_item0.push_back((int32_t)item_seq.size());
+        item_order.resize(item_seq.size());
+        for (size_t i = 0; i < item_order.size(); ++i) item_order[i] = (int32_t)i;
+        std::stable_sort(item_order.begin(), item_order.end(), [&](int32_t x, int32_t y) { return (item_np[x] & 0xffff) > (item_np[y] & 0xffff); });
+    }
+    std::vector<int32_t> pf;
+    int pf_stride = 0, pf_blocks = 0;
+    if (!decode && max_q > 64) prefill_items(c, s, n, b->q_lens, before.data(), &pf, &pf_stride, &pf_blocks);
+    Image im;
+    const size_t o_cu = im.add(cu), o_before = im.add(before), o_end = im.add(end), o_slot = im.add(slot), o_pos = im.add(pos),
+                 o_tok = im.add(tok_off), o_pt = im.add(pt), o_us = im.add(unit_seq), o_ut = im.add(unit_tok0), o_up = im.add(unit_pos0),
+                 o_uc = im.add(unit_cnt), o_is = im.add(item_seq), o_ip = im.add(item_page0), o_in = im.add(item_np), o_si = im.add(seq_item0),
+                 o_io = im.add(item_order), o_pf = im.add(pf);
+    Meta8Slot* ms = nullptr;
+    int rc = meta8_slot(c, im.total, &ms);
+    if (rc) return rc;
+    im.write(ms->host);
+    auto at = [&](size_t off) { return (const int32_t*)(ms->dev + off); };
+    ssk::Kv8Batch& k = ms->b;
+    k = {};
+    k.page_tables = at(o_pt); k.pt_stride = pt_stride;
+    k.cu_q = at(o_cu); k.before = at(o_before); k.end = at(o_end); k.slot = at(o_slot); k.pos = at(o_pos); k.tok_off = at(o_tok);
+    k.n_seqs = n; k.T = (int)T; k.max_q_len = max_q; k.max_seen = max_seen; k.seen = seen;
+    k.unit_seq = at(o_us); k.unit_tok0 = at(o_ut); k.unit_pos0 = at(o_up); k.unit_cnt = at(o_uc); k.n_units = (int)unit_seq.size();
+    k.pf_items = pf.empty() ? nullptr : at(o_pf); k.pf_stride = pf_stride; k.pf_blocks = pf_blocks;
+    k.wk.item_seq = at(o_is); k.wk.item_page0 = at(o_ip); k.wk.item_npages = at(o_in); k.wk.seq_item0 = at(o_si); k.wk.item_order = at(o_io);
+    k.wk.n_items = (int)item_seq.size(); k.wk.max_items_per_seq = max_items;
+    ms->shard = s; ms->version = s->version; ms->decode = decode; ms->write = write;
+    ms->seq_ids.assign(b->seq_ids, b->seq_ids + n);
+    ms->q_lens.assign(b->q_lens, b->q_lens + n);
+    ms->before = std::move(before); ms->end = std::move(end); ms->pos = std::move(pos);
+    *out = ms;
+    return SS_OK;
+}
+
+int run_attn8(ss_ctx* c, Shard* s, int ll, Meta8Slot* ms, bool decode, const void* q, int64_t q_stride, void* out, hipStream_t st) {
+    const int d = c->m.head_dim;
+    const ssk::Kv8Layer& kv = s->kv8_layers[ll];
+    if (!decode) {
+        ProfScope ps(c, 1, st);
+        K_TRY(c, SSK_CALL(c, attn8_prefill, q, q_stride, out, s->nq_l, s->nkv_l, d, ms->b, kv, c->force_generic, st));
+        return SS_OK;
+    }
+    const int rc = ensure_buf(c, c->ws_scratch, sizeof(float) * ssk::attn8_decode_scratch_floats(ms->b, s->nq_l, d, s->kv8_weights));
+    if (rc) return rc;
+    ProfScope ps(c, 2, st);
+    K_TRY(c, SSK_CALL(c, attn8_decode, q, q_stride, out, s->nq_l, s->nkv_l, d, ms->b, kv, (float*)c->ws_scratch.p, c->force_generic, st));
+    return SS_OK;
+}
+
+// run_attn_phase over a cache in 8 bits
+int run_attn_phase8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, const void* x_in, void* out, bool residual, hipStream_t st) {
+    const ss_model_cfg& m = c->m;
+    const LayerW& w = s->w[ll];
+    int rc = refuse_capture(c, st);
+    if (rc) return rc;
+    Meta8Slot* ms = nullptr;
+    if ((rc = prepare8(c, s, ll, b, decode, true, &ms))) return rc;
+    const int T = ms->b.T, H = m.hidden, d = m.head_dim;
+    const int nqkv = (s->nq_l + 2 * s->nkv_l) * d;
+    const size_t qkv_bytes = align256((size_t)T * nqkv * c->es);
+    if ((rc = ensure_buf(c, c->ws_qkv, qkv_bytes + (size_t)T * sizeof(float)))) return rc;
+    float* rs = (float*)((uint8_t*)c->ws_qkv.p + qkv_bytes);
+    if ((rc = ensure_buf(c, c->ws_attn, (size_t)T * s->nq_l * d * c->es))) return rc;
+    SplitWs ws;
+    if ((rc = splitk_ws(c, T, &ws))) return rc;
+    if ((rc = norm_gemm(c, x_in, w.wqkv_t, c->ws_qkv.p, nqkv, T, nqkv, ssk::EPI_STORE, rs, ws, st, ms->pending ? ms->job : ssk::UploadJob()))) return rc;
+    ms->pending = false;
+    const uint8_t* qkv = (const uint8_t*)c->ws_qkv.p;
+    {
+        ProfScope ps(c, 4, st);
+        K_TRY(c, SSK_CALL(c, kv8_rope, c->ws_qkv.p, s->nq_l, s->nkv_l, d, c->d_rope, ms->b, st));
+        K_TRY(c, SSK_CALL(c, kv8_write, qkv + (size_t)s->nq_l * d * c->es, nqkv, qkv + (size_t)(s->nq_l + s->nkv_l) * d * c->es, nqkv, s->nkv_l, d,
+                          ms->b, s->kv8_layers[ll], st));
+    }
+    if ((rc = run_attn8(c, s, ll, ms, decode, qkv, nqkv, c->ws_attn.p, st))) return rc;
+    {
+        ProfScope ps(c, 0, st);
+        K_TRY(c, SSK_CALL(c, gemm_nt, c->ws_attn.p, s->nq_l * d, w.wo_t, out, H, residual ? x_in : nullptr, T, H,
+                              s->nq_l * d, residual ? ssk::EPI_RESIDUAL : ssk::EPI_STORE, c->force_generic, st, ws.p, ws.bytes, c->gemm_rounds));
+    }
+    return mark_meta8_used(c, ms, st);
+}
+
 int run_mlp_phase(ss_ctx* c, Shard* s, int ll, int T, const void* x1, void* out, bool residual, hipStream_t st) {
     const ss_model_cfg& m = c->m;
     const LayerW& w = s->w[ll];
@@ -1010,13 +1382,14 @@ int layer_call(ss_ctx* c, const ss_shard_desc* d, int layer, int phase, const ss
         std::lock_guard<std::mutex> lk(c->mu);
         c->gemm_rounds = c->jobs_done < c->jobs_issued ? c->gemm_rounds_busy : c->gemm_rounds_idle;
     }
-    if (ph == SS_ATTN) return run_attn_phase(c, s, ll, b, decode, x_in, out, residual, st);
+    const auto attn_phase = s->kv8 ? run_attn_phase8 : run_attn_phase;
+    if (ph == SS_ATTN) return attn_phase(c, s, ll, b, decode, x_in, out, residual, st);
     if (ph == SS_MLP) {
         if (T <= 0 || T > (1 << 30)) return fail(c, SS_EINVAL, "bad token count");
         return run_mlp_phase(c, s, ll, (int)T, x_in, out, residual, st);
     }
     if ((rc = ensure_buf(c, c->ws_x1, (size_t)T * c->m.hidden * c->es))) return rc;
-    if ((rc = run_attn_phase(c, s, ll, b, decode, x_in, c->ws_x1.p, true, st))) return rc;
+    if ((rc = attn_phase(c, s, ll, b, decode, x_in, c->ws_x1.p, true, st))) return rc;
     return run_mlp_phase(c, s, ll, (int)T, c->ws_x1.p, out, true, st);
 }
 
@@ -1069,7 +1442,7 @@ size_t build_units(ss_ctx* c, Shard* s, const std::vector<SeqJob>& seqs, const s
     }
     auto al = [](size_t x) { return (x + 63) & ~(size_t)63; };
     const size_t o_off = 0, o_len = o_off + al(8 * n), o_pt = o_len + al(4 * n), o_layer = o_pt + al(4 * n);
-    const size_t o_pages = o_layer + al(4 * n), total = o_pages + al(4 * n_pages);
+    const size_t o_slot = o_layer + al(4 * n), o_pages = o_slot + (s->kv8 ? al(4 * n) : 0), total = o_pages + al(4 * n_pages);
     if (total > cap) return 0;
     int64_t* uoff = (int64_t*)(h + o_off);
     int32_t* ulen = (int32_t*)(h + o_len);
@@ -1088,6 +1461,7 @@ size_t build_units(ss_ctx* c, Shard* s, const std::vector<SeqJob>& seqs, const s
         ulen[u - u0] = sj.len;
         upt[u - u0] = (int32_t)pt_off[units[u].seq_idx];
         ulay[u - u0] = units[u].ll;
+        if (s->kv8) ((int32_t*)(h + o_slot))[u - u0] = sj.slot;
         off_elems += units[u].bytes / c->es;
         max_pages = std::max(max_pages, (sj.len + c->m.page_size - 1) / c->m.page_size);
     }
@@ -1098,7 +1472,7 @@ size_t build_units(ss_ctx* c, Shard* s, const std::vector<SeqJob>& seqs, const s
     ru->pages = (const int32_t*)(dbase + o_pages);
     ru->n_units = (int)n;
     ru->max_pages = max_pages;
-    (void)s;
+    ru->unit_slot = s->kv8 ? (const int32_t*)(dbase + o_slot) : nullptr;
     return total;
 }
 
@@ -1227,8 +1601,7 @@ int worker_job(ss_ctx* c, Lane& L, Job& job) {
         HIP_TRY(c, hipMemcpyAsync(L.mv_meta_dev, L.mv_meta_host, mbytes, hipMemcpyHostToDevice, L.side));
         if (job.dir == SS_OUT) {
             ProfScope ps(c, 3, L.side);
-            K_TRY(c, SSK_CALL(c, kv_gather, s->d_k_pools, s->d_v_pools, s->nkv_l, c->m.head_dim, c->m.page_size, ru,
-                                    L.dev_staging, L.side));
+            K_TRY(c, repack(c, s, false, ru, L.dev_staging, L.side));
         }
         // runs of this group: (unit, K|V) -> contiguous in staging and in the tier
         size_t min_run = SIZE_MAX;
@@ -1353,8 +1726,7 @@ int worker_job(ss_ctx* c, Lane& L, Job& job) {
         }
         if (job.dir == SS_IN) {
             ProfScope ps(c, 3, L.side);
-            K_TRY(c, SSK_CALL(c, kv_scatter, s->d_k_pools, s->d_v_pools, s->nkv_l, c->m.head_dim, c->m.page_size, ru,
-                                     L.dev_staging, L.side));
+            K_TRY(c, repack(c, s, true, ru, L.dev_staging, L.side));
         }
         g0 = g1;
     }
@@ -1434,6 +1806,39 @@ void wait_idle(ss_ctx* c) {
     c->cv_idle.wait(lk, [&] {
         return c->lane[0].jobs.empty() && !c->lane[0].busy && c->lane[1].jobs.empty() && !c->lane[1].busy;
     });
+}
+
+// Calls fn(units, bytes in front of them) for the units' page lists, as many at a time as the images hold, on `st`.
+// Into pages and out again, 64 prompts over ten layers: 2219 us when each call waited for the stream, cleared eight
+// megabytes and copied, 2074 us like this.  The page lists are worked out while the stream is busy and uploaded by a kernel in front of the one
+// that reads them: from two page-locked images in turn, each rewritten once the kernels of its last use are through.
+template <class F>
+int over_units(ss_ctx* c, Shard* s, const std::vector<SeqJob>& seqs, const std::vector<Unit>& units, hipStream_t st, F fn) {
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;         // a captured graph cannot hold the call: the page
+    HIP_TRY(c, hipStreamIsCapturing(st, &cap));                      // lists are those of now
+    if (cap != hipStreamCaptureStatusNone) return fail(c, SS_EHIP, "device-side export / import: the stream is capturing");
+    wait_idle(c);   // pages that a mover still writes are exported as they will be, pages it still reads not overwritten
+    size_t stage_off = 0;
+    for (size_t u0 = 0; u0 < units.size(); u0 += 32768) {
+        const size_t u1 = std::min(units.size(), u0 + 32768);
+        XferSlot& x = c->xfer[c->xfer_next];
+        c->xfer_next ^= 1;
+        HIP_TRY(c, hipEventSynchronize(x.done));
+        ssk::RepackUnits ru{};
+        const size_t mbytes = build_units(c, s, seqs, units, u0, u1, x.host, x.dev, c->xfer_cap, &ru);
+        if (!mbytes) return fail(c, SS_ENOMEM, "repack metadata region too small");
+        void* mapped = nullptr;
+        HIP_TRY(c, hipHostGetDevicePointer(&mapped, x.host, 0));
+        HIP_TRY(c, ssk::upload(mapped, x.dev, mbytes, st));
+        {
+            ProfScope ps(c, 3, st);
+            const hipError_t e = fn(ru, stage_off);
+            HIP_TRY(c, hipEventRecord(x.done, st));
+            K_TRY(c, e);
+        }
+        for (size_t u = u0; u < u1; ++u) stage_off += units[u].bytes;
+    }
+    return SS_OK;
 }
 
 int upload_matrix(ss_ctx* c, const void* src, int location, size_t bytes, void** tmp_out, const void** dev_src) {
@@ -1771,6 +2176,7 @@ int ss_destroy(ss_ctx* c) {
         }
         for (void* p : s->k_pool) if (p) (void)hipFree(p);
         for (void* p : s->v_pool) if (p) (void)hipFree(p);
+        for (void* p : s->kv8_mem) (void)hipFree(p);
         if (s->d_k_pools) (void)hipFree(s->d_k_pools);
         if (s->d_v_pools) (void)hipFree(s->d_v_pools);
         if (s->w_ready) (void)hipEventDestroy(s->w_ready);
@@ -1780,6 +2186,11 @@ int ss_destroy(ss_ctx* c) {
                       &c->ws_chain[0], &c->ws_chain[1]})
         if (b->p) (void)hipFree(b->p);
     for (auto& ms : c->meta) {
+        if (ms.host) (void)hipHostFree(ms.host);
+        if (ms.dev) (void)hipFree(ms.dev);
+        if (ms.done) (void)hipEventDestroy(ms.done);
+    }
+    for (auto& ms : c->meta8) {
         if (ms.host) (void)hipHostFree(ms.host);
         if (ms.dev) (void)hipFree(ms.dev);
         if (ms.done) (void)hipEventDestroy(ms.done);
@@ -2058,6 +2469,10 @@ static int kv_swap(ss_ctx* c, const ss_shard_desc* d, int dir, const int64_t* se
         for (int i = 0; i < n; ++i) {
             auto it = s->seqs.find(seq_ids[i]);
             if (it == s->seqs.end()) return fail(c, SS_ENOENT, "sequence %lld not resident in this shard", (long long)seq_ids[i]);
+            if ((rc = kv8_whole(c, s, seq_ids[i], it->second))) return rc;
+            if (it->second.evicted)
+                return fail(c, SS_EINVAL, "sequence %lld has lost %d tokens to eviction: its positions would be lost in the tier",
+                            (long long)seq_ids[i], it->second.evicted);
             auto ts = c->tier_slots.find(seq_ids[i]);
             if (ts != c->tier_slots.end() && ts->second.len != it->second.len)
                 return fail(c, SS_EINVAL, "sequence %lld is in the tier with length %d, shard holds %d",
@@ -2083,7 +2498,7 @@ static int kv_swap(ss_ctx* c, const ss_shard_desc* d, int dir, const int64_t* se
         }
         for (int i = 0; i < n; ++i) {
             const SeqState& st = s->seqs[seq_ids[i]];
-            job.seqs.push_back({seq_ids[i], st.len, st.pages, c->tier_slots[seq_ids[i]].off});
+            job.seqs.push_back({seq_ids[i], st.len, st.pages, c->tier_slots[seq_ids[i]].off, st.slot});
         }
     } else {
         for (int i = 0; i < n; ++i) {
@@ -2104,8 +2519,9 @@ static int kv_swap(ss_ctx* c, const ss_shard_desc* d, int dir, const int64_t* se
         for (int i = 0; i < n; ++i) {
             const TierSlot& ts = c->tier_slots[seq_ids[i]];
             if ((rc = ensure_pages(c, s, seq_ids[i], ts.len))) return rc;
-            const SeqState& st = s->seqs[seq_ids[i]];
-            job.seqs.push_back({seq_ids[i], ts.len, st.pages, ts.off});
+            SeqState& st = s->seqs[seq_ids[i]];
+            kv8_arrived(s, st);
+            job.seqs.push_back({seq_ids[i], ts.len, st.pages, ts.off, st.slot});
         }
     }
     if (out_id && dir == SS_OUT) job.followed = true;
@@ -2177,6 +2593,7 @@ int ss_kv_free(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, int n)
         auto it = s->seqs.find(seq_ids[i]);
         if (it == s->seqs.end()) continue;   // listed twice
         for (int32_t p : it->second.pages) s->free_pages.push(p);
+        if (it->second.slot >= 0) s->free_slots.push(it->second.slot);
         s->seqs.erase(it);
     }
     s->version++;
@@ -2219,47 +2636,23 @@ static int xfer_dev(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, c
         if ((rc = check_new_seqs_fit(c, s, lens, n))) return rc;
         for (int i = 0; i < n; ++i) {
             if ((rc = ensure_pages(c, s, seq_ids[i], lens[i]))) return rc;
-            seqs.push_back({seq_ids[i], lens[i], s->seqs[seq_ids[i]].pages, 0});
+            SeqState& sst = s->seqs[seq_ids[i]];
+            kv8_arrived(s, sst);
+            seqs.push_back({seq_ids[i], lens[i], sst.pages, 0, sst.slot});
         }
     } else {
         for (int i = 0; i < n; ++i) {
             auto it = s->seqs.find(seq_ids[i]);
             if (it == s->seqs.end()) return fail(c, SS_ENOENT, "sequence %lld not resident", (long long)seq_ids[i]);
-            seqs.push_back({seq_ids[i], it->second.len, it->second.pages, 0});
+            if ((rc = kv8_whole(c, s, seq_ids[i], it->second))) return rc;
+            seqs.push_back({seq_ids[i], it->second.len, it->second.pages, 0, it->second.slot});
         }
     }
     const std::vector<Unit> units = make_units(c, s, seqs);
     hipStream_t st = (hipStream_t)stream;
-    // Into pages and out again, 64 prompts over ten layers: 2219 us when each call waited for the stream, cleared eight
-    // megabytes and copied, 2074 us like this.  The page lists are worked out while the stream is busy and uploaded by a kernel in front of the one
-    // that reads them: from two page-locked images in turn, each rewritten once the kernels of its last use are through.
-    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;         // a captured graph cannot hold the call: the page
-    HIP_TRY(c, hipStreamIsCapturing(st, &cap));                      // lists are those of now
-    if (cap != hipStreamCaptureStatusNone) return fail(c, SS_EHIP, "device-side export / import: the stream is capturing");
-    wait_idle(c);   // pages that a mover still writes are exported as they will be, pages it still reads not overwritten
-    size_t stage_off = 0;
-    for (size_t u0 = 0; u0 < units.size(); u0 += 32768) {
-        const size_t u1 = std::min(units.size(), u0 + 32768);
-        XferSlot& x = c->xfer[c->xfer_next];
-        c->xfer_next ^= 1;
-        HIP_TRY(c, hipEventSynchronize(x.done));
-        ssk::RepackUnits ru{};
-        const size_t mbytes = build_units(c, s, seqs, units, u0, u1, x.host, x.dev, c->xfer_cap, &ru);
-        if (!mbytes) return fail(c, SS_ENOMEM, "repack metadata region too small");
-        void* mapped = nullptr;
-        HIP_TRY(c, hipHostGetDevicePointer(&mapped, x.host, 0));
-        HIP_TRY(c, ssk::upload(mapped, x.dev, mbytes, st));
-        uint8_t* stg = (uint8_t*)staging + stage_off;
-        {
-            ProfScope ps(c, 3, st);
-            hipError_t e = import ? SSK_CALL(c, kv_scatter, s->d_k_pools, s->d_v_pools, s->nkv_l, c->m.head_dim, c->m.page_size, ru, stg, st)
-                                  : SSK_CALL(c, kv_gather, s->d_k_pools, s->d_v_pools, s->nkv_l, c->m.head_dim, c->m.page_size, ru, stg, st);
-            HIP_TRY(c, hipEventRecord(x.done, st));
-            K_TRY(c, e);
-        }
-        for (size_t u = u0; u < u1; ++u) stage_off += units[u].bytes;
-    }
-    return SS_OK;
+    return over_units(c, s, seqs, units, st, [&](const ssk::RepackUnits& ru, size_t off) {
+        return repack(c, s, import, ru, (uint8_t*)staging + off, st);
+    });
 }
 
 int ss_kv_export_dev(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, int n, void* staging, void* stream) {
@@ -2269,6 +2662,200 @@ int ss_kv_export_dev(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, 
 int ss_kv_import_dev(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, const int32_t* lens, int n,
                      const void* staging, void* stream) {
     return xfer_dev(c, d, seq_ids, lens, n, const_cast<void*>(staging), stream, true);
+}
+
+// ---- caches in 8 bits
+namespace {
+
+// The context's device for the length of a call.
+struct DeviceScope {
+    int before = -1;
+    bool ok = false;
+    explicit DeviceScope(int device) {
+        if (hipGetDevice(&before) != hipSuccess) { before = -1; return; }
+        ok = before == device || hipSetDevice(device) == hipSuccess;
+        if (before == device) before = -1;
+    }
+    ~DeviceScope() { if (before >= 0) (void)hipSetDevice(before); }
+};
+
+int kv8_shard(ss_ctx* c, const ss_shard_desc* d, Shard** out) {
+    int rc = get_shard(c, d, out);
+    if (rc) return rc;
+    if (!(*out)->kv8) return fail(c, SS_EINVAL, "the shard's cache is not kept in 8 bits (ss_kv8_enable)");
+    return SS_OK;
+}
+
+// what: 0 write, 1 prefill, 2 decode
+int kv8_call(ss_ctx* c, const ss_shard_desc* d, int layer, const ss_batch* b, const ss_qkv* x, void* out, void* stream, int what) {
+    if (!c) return SS_EINVAL;
+    if (!b || !x || b->n_seqs <= 0 || !b->seq_ids || !b->q_lens || !b->kv_lens_before || (what && (!x->q || !out)))
+        return fail(c, SS_EINVAL, "null or empty batch / buffers");
+    if (!x->k != !x->v || (!what && !x->k)) return fail(c, SS_EINVAL, "keys and values come together");
+    DeviceScope dev(c->rt.device);
+    if (!dev.ok) return fail(c, SS_EHIP, "device %d cannot be made current", c->rt.device);
+    Shard* s = nullptr;
+    int rc = kv8_shard(c, d, &s);
+    if (rc) return rc;
+    if (layer < d->layer_begin || layer >= d->layer_end)
+        return fail(c, SS_EINVAL, "layer %d outside the shard's range [%d,%d)", layer, d->layer_begin, d->layer_end);
+    const int hd = c->m.head_dim, piece = 16 / (int)c->es;
+    const bool write = x->k != nullptr;
+    if (((uintptr_t)x->q | (uintptr_t)x->k | (uintptr_t)x->v | (uintptr_t)out) % 16)
+        return fail(c, SS_EINVAL, "q, k, v and out have to be 16-byte aligned");
+    auto rows = [&](const char* name, int64_t stride, int heads) -> int {
+        if (stride < (int64_t)heads * hd || stride % piece)
+            return fail(c, SS_EINVAL, "%s: tokens %lld elements apart, at least %d and a multiple of %d are needed", name, (long long)stride, heads * hd, piece);
+        return SS_OK;
+    };
+    if (what && (rc = rows("q", x->q_stride, s->nq_l))) return rc;
+    if (write && ((rc = rows("k", x->k_stride, s->nkv_l)) || (rc = rows("v", x->v_stride, s->nkv_l)))) return rc;
+    if (what && s->nq_l % s->nkv_l) return fail(c, SS_EINVAL, "%d query heads over %d kv heads", s->nq_l, s->nkv_l);
+    hipStream_t st = (hipStream_t)stream;
+    if ((rc = refuse_capture(c, st))) return rc;
+    if ((rc = ensure_pools(c, s))) return rc;
+    Meta8Slot* ms = nullptr;
+    const int ll = layer - d->layer_begin;
+    if ((rc = prepare8(c, s, ll, b, what == 2, write, &ms))) return rc;
+    if (ms->pending) {
+        HIP_TRY(c, ssk::upload(ms->job.src, ms->job.dst, (size_t)ms->job.n16 * 16, st));
+        ms->pending = false;
+    }
+    if (write) {
+        ProfScope ps(c, 4, st);
+        K_TRY(c, SSK_CALL(c, kv8_write, x->k, x->k_stride, x->v, x->v_stride, s->nkv_l, hd, ms->b, s->kv8_layers[ll], st));
+    }
+    if (what && (rc = run_attn8(c, s, ll, ms, what == 2, x->q, x->q_stride, out, st))) return rc;
+    return mark_meta8_used(c, ms, st);
+}
+
+}  // namespace
+
+int ss_kv8_enable(ss_ctx* c, const ss_shard_desc* d, const ss_kv8_cfg* cfg) {
+    if (!c) return SS_EINVAL;
+    if (!cfg || cfg->max_seqs <= 0) return fail(c, SS_EINVAL, "a cache in 8 bits needs room for a sequence");
+    Shard* s = nullptr;
+    int rc = get_shard(c, d, &s);
+    if (rc) return rc;
+    if (s->pools_ready || s->kv8) return fail(c, SS_EINVAL, "the shard's pages are in use");
+    s->kv8 = true;
+    s->kv8_slots = cfg->max_seqs;
+    s->kv8_weights = cfg->weights != 0;
+    return SS_OK;
+}
+
+int ss_kv8_write(ss_ctx* c, const ss_shard_desc* d, int layer, const ss_batch* b, const ss_qkv* x, void* stream) {
+    return kv8_call(c, d, layer, b, x, nullptr, stream, 0);
+}
+
+int ss_kv8_attn_prefill(ss_ctx* c, const ss_shard_desc* d, int layer, const ss_batch* b, const ss_qkv* x, void* out, void* stream) {
+    return kv8_call(c, d, layer, b, x, out, stream, 1);
+}
+
+int ss_kv8_attn_decode(ss_ctx* c, const ss_shard_desc* d, int layer, const ss_batch* b, const ss_qkv* x, void* out, void* stream) {
+    return kv8_call(c, d, layer, b, x, out, stream, 2);
+}
+
+int ss_kv8_weights(ss_ctx* c, const ss_shard_desc* d, int dir, const int64_t* seq_ids, int n, float* buf, void* stream) {
+    if (!c) return SS_EINVAL;
+    if (n < 0 || (n > 0 && (!seq_ids || !buf))) return fail(c, SS_EINVAL, "bad arguments");
+    if (dir != SS_OUT && dir != SS_IN) return fail(c, SS_EINVAL, "bad direction %d", dir);
+    DeviceScope dev(c->rt.device);
+    if (!dev.ok) return fail(c, SS_EHIP, "device %d cannot be made current", c->rt.device);
+    Shard* s = nullptr;
+    int rc = kv8_shard(c, d, &s);
+    if (rc) return rc;
+    if (!s->kv8_weights) return fail(c, SS_EINVAL, "the shard keeps no attention weights");
+    std::vector<SeqJob> seqs;
+    std::vector<Unit> units;
+    for (int i = 0; i < n; ++i) {
+        auto it = s->seqs.find(seq_ids[i]);
+        if (it == s->seqs.end()) return fail(c, SS_ENOENT, "sequence %lld not resident", (long long)seq_ids[i]);
+        if ((rc = kv8_whole(c, s, seq_ids[i], it->second))) return rc;
+        for (int j = 0; dir == SS_IN && j < i; ++j)
+            if (seq_ids[j] == seq_ids[i]) return fail(c, SS_EINVAL, "sequence %lld is listed twice", (long long)seq_ids[i]);
+        seqs.push_back({seq_ids[i], it->second.len, it->second.pages, 0, it->second.slot});
+        // counted in elements of the model's type, of which over_units takes as many as there are weights
+        for (int ll = 0; ll < s->n_layers_l; ++ll) units.push_back({i, ll, (size_t)s->nkv_l * it->second.len * c->es});
+    }
+    hipStream_t st = (hipStream_t)stream;
+    return over_units(c, s, seqs, units, st, [&](const ssk::RepackUnits& ru, size_t off) {
+        return ssk::kv8_weights(s->d_kv8_layers, s->nkv_l, ru, buf + off / c->es, dir == SS_IN, st);
+    });
+}
+
+int ss_kv8_evict(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, const int32_t* keep, int n, int recent, void* stream) {
+    if (!c) return SS_EINVAL;
+    if (n < 0 || (n > 0 && (!seq_ids || !keep)) || recent < 0) return fail(c, SS_EINVAL, "bad arguments");
+    DeviceScope dev(c->rt.device);
+    if (!dev.ok) return fail(c, SS_EHIP, "device %d cannot be made current", c->rt.device);
+    Shard* s = nullptr;
+    int rc = kv8_shard(c, d, &s);
+    if (rc) return rc;
+    if (!s->kv8_weights) return fail(c, SS_EINVAL, "the shard keeps no attention weights");
+    hipStream_t st = (hipStream_t)stream;
+    if ((rc = refuse_capture(c, st))) return rc;
+    std::vector<SeqState*> sts;
+    std::vector<int32_t> lens, keeps, slots;
+    std::vector<int64_t> offs;
+    int64_t total = 0;
+    int pt_stride = 1, max_len = 0;
+    ++c->batches;
+    for (int i = 0; i < n; ++i) {
+        auto it = s->seqs.find(seq_ids[i]);
+        if (it == s->seqs.end()) return fail(c, SS_ENOENT, "sequence %lld not resident", (long long)seq_ids[i]);
+        SeqState& q = it->second;
+        if (q.seen == c->batches) return fail(c, SS_EINVAL, "sequence %lld is listed twice", (long long)seq_ids[i]);
+        q.seen = c->batches;
+        if (keep[i] < 1) return fail(c, SS_EINVAL, "sequence %lld cannot be cut to %d tokens", (long long)seq_ids[i], keep[i]);
+        if ((rc = kv8_whole(c, s, seq_ids[i], q))) return rc;
+        if (q.len <= keep[i]) continue;
+        sts.push_back(&q);
+        lens.push_back(q.len);
+        keeps.push_back(keep[i]);
+        slots.push_back(q.slot);
+        offs.push_back(total);
+        total += (int64_t)s->n_layers_l * s->nkv_l * keep[i];
+        pt_stride = std::max<int>(pt_stride, (int)q.pages.size());
+        max_len = std::max(max_len, q.len);
+    }
+    const int m = (int)sts.size();
+    if (!m) return SS_OK;
+    wait_seqs_idle(c, s, seq_ids, n);                       // movements still read what is moved here
+    if ((rc = ensure_buf(c, c->ws_scratch, sizeof(int32_t) * (size_t)total))) return rc;
+    std::vector<int32_t> pt((size_t)m * pt_stride, 0);
+    for (int i = 0; i < m; ++i) std::copy(sts[i]->pages.begin(), sts[i]->pages.end(), pt.begin() + (size_t)i * pt_stride);
+    Image im;
+    const size_t o_len = im.add(lens), o_keep = im.add(keeps), o_slot = im.add(slots), o_off = im.add(offs), o_pt = im.add(pt);
+    Meta8Slot* ms = nullptr;
+    if ((rc = meta8_slot(c, im.total, &ms))) return rc;
+    im.write(ms->host);
+    ms->pending = false;
+    HIP_TRY(c, ssk::upload(ms->job.src, ms->job.dst, (size_t)ms->job.n16 * 16, st));
+    ssk::Kv8Evict e{};
+    e.page_tables = (const int32_t*)(ms->dev + o_pt);
+    e.pt_stride = pt_stride;
+    e.len = (const int32_t*)(ms->dev + o_len);
+    e.keep = (const int32_t*)(ms->dev + o_keep);
+    e.slot = (const int32_t*)(ms->dev + o_slot);
+    e.list_off = (const int64_t*)(ms->dev + o_off);
+    e.n_seqs = m; e.n_layers = s->n_layers_l; e.recent = recent; e.max_len = max_len;
+    {
+        ProfScope ps(c, 3, st);
+        K_TRY(c, SSK_CALL(c, kv8_evict, s->d_kv8_layers, s->nkv_l, c->m.head_dim, e, (int32_t*)c->ws_scratch.p, st));
+    }
+    for (int i = 0; i < m; ++i) {
+        SeqState& q = *sts[i];
+        q.evicted += q.len - keeps[i];
+        q.len = q.floor = keeps[i];
+        std::fill(q.layer_len.begin(), q.layer_len.end(), q.len);
+        while (q.pages.size() > (size_t)(q.len + 15) / 16) {
+            s->free_pages.push(q.pages.back());
+            q.pages.pop_back();
+        }
+    }
+    s->version++;
+    return mark_meta8_used(c, ms, st);
 }
 
 int ss_kv_page_table(ss_ctx* c, const ss_shard_desc* d, int64_t seq, int32_t* pages, int32_t* n_inout) {
@@ -2306,7 +2893,8 @@ int ss_kv_read(ss_ctx* c, const ss_shard_desc* d, int64_t seq, int layer, void* 
     if (!s->pools_ready) return fail(c, SS_ENOENT, "shard has no cache yet");
     wait_idle(c);
     HIP_TRY(c, hipDeviceSynchronize());
-    std::vector<SeqJob> seqs{{seq, it->second.len, it->second.pages, 0}};
+    if ((rc = kv8_whole(c, s, seq, it->second))) return rc;
+    std::vector<SeqJob> seqs{{seq, it->second.len, it->second.pages, 0, it->second.slot}};
     std::vector<Unit> units{{0, layer - d->layer_begin, (size_t)2 * s->nkv_l * it->second.len * c->m.head_dim * c->es}};
     std::vector<uint8_t> img(1 << 20);
     ssk::RepackUnits ru{};
@@ -2315,7 +2903,7 @@ int ss_kv_read(ss_ctx* c, const ss_shard_desc* d, int64_t seq, int layer, void* 
     HIP_TRY(c, hipMemcpy(c->lane[0].mv_meta_dev, img.data(), mbytes, hipMemcpyHostToDevice));
     void* tmp = nullptr;
     HIP_TRY(c, hipMalloc(&tmp, units[0].bytes));
-    hipError_t e = SSK_CALL(c, kv_gather, s->d_k_pools, s->d_v_pools, s->nkv_l, c->m.head_dim, c->m.page_size, ru, tmp, 0);
+    hipError_t e = repack(c, s, false, ru, tmp, 0);
     if (e == hipSuccess) e = hipMemcpy(host_out, tmp, units[0].bytes, hipMemcpyDeviceToHost);
     (void)hipFree(tmp);
     if (e != hipSuccess) return fail(c, SS_EHIP, "kv read: %s", hipGetErrorString(e));
