@@ -120,6 +120,326 @@ hipError_t attn8_prefill(int dt, const void* q, int64_t q_stride, void* out, int
     return attn8_generic(dt, q, q_stride, out, n_q, n_kv, d, b, kv, nullptr, nullptr, s);
 }
 
+// ---------------------------------------------------------------- operands of the matrix cores
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
+union Frag8 {
+    half8_t v;
+    vec16 q;
+    uint32_t w[4];
+};
+
+// Four signed bytes as four numbers of the 16-bit type, exact.  bf16: a conversion that picks its byte, and the upper halves of two
+// results put together, six operations; half: 1024 + 128 + byte has the byte in its lowest bits, five.
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+#ifdef SS_HALF_F16
+    typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+    const uint32_t u = w ^ 0x80808080u;
+    const h2_t off = {(_Float16)-1152.f, (_Float16)-1152.f};
+    lo = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x07010700u)) + off);
+    hi = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x07030702u)) + off);
+#else
+    const float f0 = (float)(int8_t)w, f1 = (float)(int8_t)(w >> 8), f2 = (float)(int8_t)(w >> 16), f3 = (float)(int8_t)(w >> 24);
+    lo = __builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u);
+    hi = __builtin_amdgcn_perm(__float_as_uint(f3), __float_as_uint(f2), 0x07060302u);
+#endif
+}
+__device__ __forceinline__ Frag8 widen8(uint32_t a, uint32_t b) {
+    Frag8 f;
+    widen4(a, f.w[0], f.w[1]);
+    widen4(b, f.w[2], f.w[3]);
+    return f;
+}
+
+// The weights of a block are kept times its V step: the second product then takes V's whole numbers as they are, and a 16-bit
+// weight is rounded relative to what it contributes.  lv: log 2 of the step; inv brings the sum of such weights back.  A block of
+// zeros adds to the sum alone: any step serves, this one lies below those of half values and far above underflow.  Steps below
+// 2^-100 count as that.
+constexpr float LV_ZERO = -40.f, LV_MIN = -100.f;
+// Half: the largest weight is 2^14 instead of 1, so that those of 2^-28 of it are still in the type's normal range.  With 1 a token
+// of weight 2^-16 is rounded to 2^-9 of itself, which shows in outputs whose heavy tokens happen to have a value of 0.
+#ifdef SS_HALF_F16
+constexpr float TOP_EXP = 14.f;
+#else
+constexpr float TOP_EXP = 0.f;
+#endif
+__device__ __forceinline__ void v_step(float amax, float& lv, float& inv) {
+    const float step = amax / 127.f, l = __builtin_amdgcn_logf(step);
+    lv = amax == 0.f ? LV_ZERO : l < LV_MIN ? LV_MIN : l;
+    inv = exp2_fast(-lv);
+}
+
+// ---------------------------------------------------------------- single tokens
+// A wave per (work item, kv head, 16 of its query heads).  An item is pages page0, page0 + stride, ... of a sequence.  The transposed
+// products S^T = K Q^T and O^T = V^T P^T: the scores of the first are then in the registers where the second wants its weights.
+// Four pages a step: row 4 p + v of score product i is token 4 i + v of page p, so that lane group p (16 lanes) ends up with the
+// 16 scores of page p, one query a lane: one K and one V step a lane, and 16-byte loads of 16 tokens (V) or 16 elements (K),
+// half a cache line a row.  K of the next four pages is requested behind the score products of these, V of these in front of them.
+// Bound by the page reads.
+template <int D, bool WEIGHTS>
+__global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restrict__ q, int64_t q_stride, int n_q, int n_kv, int n_ct,
+                                                          Kv8Batch b, Kv8Layer kv, float* __restrict__ scratch, float* __restrict__ scores,
+                                                          float scale_log2e) {
+    constexpr int HB = D / 64, DT = D / 16;
+    const int heads = n_kv * n_ct;
+    const int item = b.wk.item_order[blockIdx.x / heads], g = blockIdx.x % heads / n_ct, ct = blockIdx.x % n_ct;
+    const int G = n_q / n_kv;
+    const int sq = b.wk.item_seq[item], page0 = b.wk.item_page0[item], np = b.wk.item_npages[item];
+    const int npg = np & 0xffff, stride = (int)((unsigned)np >> 16);
+    const int p = b.before[sq], full = b.end[sq] / 16;
+    const int lane = threadIdx.x, lq = lane & 15, g4 = lane >> 4;
+    const bool open_here = page0 + (npg - 1) * stride >= full;           // the item's last page is the open block
+    const int npc = npg - open_here;
+    const bool mine = ct * 16 + lq < G;
+    const int a = g * G + ct * 16 + lq;
+
+    Frag8 qf[HB][2];
+#pragma unroll
+    for (int h = 0; h < HB; ++h)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            qf[h][j].w[0] = qf[h][j].w[1] = qf[h][j].w[2] = qf[h][j].w[3] = 0u;
+            if (mine) qf[h][j].q = *reinterpret_cast<const vec16*>(q + (int64_t)b.cu_q[sq] * q_stride + (size_t)a * D + 64 * h + 16 * g4 + 8 * j);
+        }
+    f32x4_t o[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float r = -INFINITY, l = 0.f;                                        // reference of the exponents, sum in its units
+    float* sp = WEIGHTS ? scores + (size_t)b.tok_off[sq] * n_q + a : nullptr;
+
+    auto rescale = [&](float top) {
+        const float alpha = exp2_fast(r - top);
+        r = top;
+        l *= alpha;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[t][v] *= alpha;
+    };
+    auto over_groups = [&](float x) {
+        x = fmaxf(x, __shfl_xor(x, 16, 64));
+        return fmaxf(x, __shfl_xor(x, 32, 64));
+    };
+
+    if (npc > 0) {
+        const int32_t* pt = b.page_tables + (size_t)sq * b.pt_stride + page0;
+        auto page_at = [&](int j) { return pt[(j < npc ? j : npc - 1) * stride]; };
+        struct Ids { int k, v; };
+        auto ids = [&](int j0) { return Ids{page_at(j0 + (lq >> 2)), page_at(j0 + g4)}; };
+        struct Keys { vec16 k[4][HB]; float2 amax; };
+        auto load_k = [&](const Ids& id, Keys& f) {
+            const int8_t* kp = kv.k + ((size_t)id.k * n_kv + g) * 16 * D + (lq & 3) * D + 16 * g4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int h = 0; h < HB; ++h) f.k[i][h] = *reinterpret_cast<const vec16*>(kp + 4 * i * D + 64 * h);
+            f.amax = *reinterpret_cast<const float2*>(kv.amax + ((size_t)id.v * n_kv + g) * 2);
+        };
+        auto step = [&](int j0, const Ids& cur, const Keys& f, const Ids& nxt, Keys& fn) {
+            const int8_t* vp = kv.v + ((size_t)cur.v * n_kv + g) * 16 * D + lq * 16;
+            vec16 vr[DT];
+#pragma unroll
+            for (int t = 0; t < DT; ++t) vr[t] = *reinterpret_cast<const vec16*>(vp + t * 256);
+            __builtin_amdgcn_sched_barrier(0);
+            f32x4_t s[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < HB; ++h) {
+                    s[i] = SS_MFMA_16x16x32(widen8(f.k[i][h].w[0], f.k[i][h].w[1]).v, qf[h][0].v, s[i], 0, 0, 0);
+                    s[i] = SS_MFMA_16x16x32(widen8(f.k[i][h].w[2], f.k[i][h].w[3]).v, qf[h][1].v, s[i], 0, 0, 0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            load_k(nxt, fn);
+            __builtin_amdgcn_sched_barrier(0);
+            const float ks = f.amax.x / 127.f * scale_log2e;
+            float lv, inv;
+            v_step(f.amax.y, lv, inv);
+            const int pg = page0 + (j0 + g4) * stride;
+            const int seen = j0 + g4 < npc ? p - pg * 16 : -1;           // tokens 0 .. seen of the lane's page
+            const bool whole = j0 + 4 < npc;                             // only an item's last step has hidden tokens or pages too few
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    s[i][v] = whole || 4 * i + v <= seen ? s[i][v] * ks : -INFINITY;
+                    top = fmaxf(top, s[i][v]);
+                    if (WEIGHTS && mine && 4 * i + v <= seen) sp[(size_t)(pg * 16 + 4 * i + v) * n_q] = s[i][v];
+                }
+            top = over_groups(top + lv) - TOP_EXP;
+            if (__any(top > r)) rescale(fmaxf(top, r));
+            const float off = lv - r;
+            float rs = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const float w = exp2_fast(s[i][v] + off);
+                    s[i][v] = whole || 4 * i + v <= seen ? w : 0.f;      // the step of a hidden block may not be a number
+                    rs += s[i][v];
+                }
+            l += whole || seen >= 0 ? rs * inv : 0.f;
+            Frag8 pa, pb;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                pa.w[2 * i] = pack_bf16x2(s[i][0], s[i][1]);
+                pa.w[2 * i + 1] = pack_bf16x2(s[i][2], s[i][3]);
+                pb.w[2 * i] = pack_bf16x2(s[2 + i][0], s[2 + i][1]);
+                pb.w[2 * i + 1] = pack_bf16x2(s[2 + i][2], s[2 + i][3]);
+            }
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                o[t] = SS_MFMA_16x16x32(widen8(vr[t].w[0], vr[t].w[1]).v, pa.v, o[t], 0, 0, 0);
+                o[t] = SS_MFMA_16x16x32(widen8(vr[t].w[2], vr[t].w[3]).v, pb.v, o[t], 0, 0, 0);
+            }
+        };
+        // two steps a trip, the two sets of keys in turn; page numbers are there two steps ahead.  Behind the end the last page is asked
+        // for again.
+        Ids i0 = ids(0), i1 = ids(4);
+        Keys k0, k1;
+        load_k(i0, k0);
+        for (int j = 0; j < npc; j += 8) {
+            const Ids i2 = ids(j + 8);
+            step(j, i0, k0, i1, k1);
+            const Ids i3 = ids(j + 12);
+            if (j + 4 < npc) step(j + 4, i1, k1, i2, k0);
+            i0 = i2;
+            i1 = i3;
+        }
+    }
+    if (open_here) {
+        // Tokens 4 g4 + v of the open block, in the model's type, in the first four of the group's eight slots of the second product.  V is
+        // scaled by a power of two (exact) to below 128, as the whole numbers of a full block are.
+        const int cnt = p - full * 16 + 1;
+        const bf16_t* ko = (const bf16_t*)kv.open + ((size_t)b.slot[sq] * 2 * n_kv + g) * 16 * D;
+        const bf16_t* vo = ko + (size_t)n_kv * 16 * D;
+        bf16_t raw[DT][4];
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) raw[t][v] = vo[(4 * g4 + v) * D + 16 * t + lq];
+        f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < HB; ++h)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                Frag8 kf;
+                kf.q = *reinterpret_cast<const vec16*>(ko + lq * D + 64 * h + 16 * g4 + 8 * j);
+                s = SS_MFMA_16x16x32(kf.v, qf[h][j].v, s, 0, 0, 0);
+            }
+        float big = 0.f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                if (4 * g4 + v < cnt) big = fmaxf(big, fabsf(bf2f(raw[t][v])));
+        big = wave_max(big);
+        int e = big > 0.f && big < INFINITY ? (int)(__float_as_uint(big) >> 23) - 127 - 6 : big > 0.f ? 0 : (int)LV_ZERO;
+        e = e < (int)LV_MIN ? (int)LV_MIN : e;
+        const float lv = (float)e;
+        float top = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            s[v] = 4 * g4 + v < cnt ? s[v] * scale_log2e : -INFINITY;
+            top = fmaxf(top, s[v]);
+            if (WEIGHTS && mine && 4 * g4 + v < cnt) sp[(size_t)(full * 16 + 4 * g4 + v) * n_q] = s[v];
+        }
+        rescale(fmaxf(r, over_groups(top + lv) - TOP_EXP));
+        float rs = 0.f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            s[v] = 4 * g4 + v < cnt ? exp2_fast(s[v] + (lv - r)) : 0.f;
+            rs += s[v];
+        }
+        l += rs * exp2_fast(-lv);
+        Frag8 pf;
+        pf.w[0] = pack_bf16x2(s[0], s[1]);
+        pf.w[1] = pack_bf16x2(s[2], s[3]);
+        pf.w[2] = pf.w[3] = 0u;
+        const float down = exp2_fast(-lv);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+            float x[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) x[v] = 4 * g4 + v < cnt ? bf2f(raw[t][v]) * down : 0.f;
+            Frag8 vf;
+            vf.w[0] = pack_bf16x2(x[0], x[1]);
+            vf.w[1] = pack_bf16x2(x[2], x[3]);
+            vf.w[2] = vf.w[3] = 0u;
+            o[t] = SS_MFMA_16x16x32(vf.v, pf.v, o[t], 0, 0, 0);
+        }
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (mine) {
+        float* out = scratch + ((size_t)item * n_q + a) * (D + 4);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4_t*>(out + t * 16 + 4 * g4) = o[t];
+        if (g4 == 0) { out[D] = r; out[D + 1] = l; }
+    }
+}
+
+// Merge of the items' partial results: D / 4 threads per (query head, sequence), HB heads a block; four items are requested together.
+template <int D, int HB>
+__global__ __launch_bounds__(D / 4 * HB) void attn8_merge_kernel(const float* __restrict__ scratch, bf16_t* __restrict__ out, int n_q, Kv8Batch b,
+                                                                 float* __restrict__ lse) {
+    const int sq = blockIdx.y, e = threadIdx.x % (D / 4) * 4, a = blockIdx.x * HB + threadIdx.x / (D / 4);
+    if (a >= n_q) return;
+    const int i0 = b.wk.seq_item0[sq], i1 = b.wk.seq_item0[sq + 1];
+    float M = -INFINITY, den = 0.f;
+    f32x4_t num = {0.f, 0.f, 0.f, 0.f};
+    for (int i = i0; i < i1; i += 4) {
+        float m[4], l[4];
+        f32x4_t v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float* sp = scratch + ((size_t)(i + u < i1 ? i + u : i1 - 1) * n_q + a) * (D + 4);
+            m[u] = sp[D];
+            l[u] = sp[D + 1];
+            v[u] = *reinterpret_cast<const f32x4_t*>(sp + e);
+        }
+        float mx = M;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (i + u >= i1) {                                           // repeated: weight 0 would not keep an infinite one out
+                m[u] = -INFINITY;
+                l[u] = 0.f;
+                v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            }
+            mx = fmaxf(mx, m[u]);
+        }
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        const float alpha = exp2_fast(M - ref);
+        M = mx;
+        num *= alpha;
+        den *= alpha;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float w = exp2_fast(m[u] - ref);
+            num += w * v[u];
+            den += w * l[u];
+        }
+    }
+    vec16 w;
+    w.w[0] = pack_bf16x2(num[0] / den, num[1] / den);
+    w.w[1] = pack_bf16x2(num[2] / den, num[3] / den);
+    *reinterpret_cast<uint2*>(out + (size_t)b.cu_q[sq] * ((size_t)n_q * D) + (size_t)a * D + e) = make_uint2(w.w[0], w.w[1]);
+    if (lse && e == 0) lse[(size_t)sq * n_q + a] = M + __builtin_amdgcn_logf(den);
+}
+
+template <int D>
+static void launch_decode(const void* q, int64_t q_stride, void* out, int n_q, int n_kv, const Kv8Batch& b, const Kv8Layer& kv, float* scratch,
+                          float* scores, float* lse, hipStream_t s) {
+    const int n_ct = (n_q / n_kv + 15) / 16;
+    const float sl2 = 1.4426950408889634f / sqrtf((float)D);
+    const unsigned grid = (unsigned)((long long)b.wk.n_items * n_kv * n_ct);
+    const auto kernel = scores ? attn8_decode_kernel<D, true> : attn8_decode_kernel<D, false>;
+    kernel<<<grid, 64, 0, s>>>((const bf16_t*)q, q_stride, n_q, n_kv, n_ct, b, kv, scratch, scores, sl2);
+    attn8_merge_kernel<D, 1024 / D><<<dim3((n_q * D + 1023) / 1024, b.n_seqs), 256, 0, s>>>(scratch, (bf16_t*)out, n_q, b, lse);
+}
+
 // ---------------------------------------------------------------- accumulated weights
 // A thread per (token, kv head): the weights of the head's G queries, in their order, onto what is there.
 __global__ __launch_bounds__(256) void attn8_weights_kernel(const float* __restrict__ scores, const float* __restrict__ lse, int n_q, int n_kv,
@@ -145,10 +465,17 @@ hipError_t attn8_decode(int dt, const void* q, int64_t q_stride, void* out, int 
     if (b.n_seqs <= 0) return hipSuccess;
     if (!attn8_fits(n_q, n_kv, d, b, q, q_stride, dt) || b.max_q_len != 1 || !scratch) return hipErrorInvalidValue;
     if ((long long)b.max_seen * n_kv > 0x7fffff00ll) return hipErrorInvalidValue;
-    (void)force_generic;
     float* lse = kv.w ? scratch + partial_floats(b, n_q, d) : nullptr;
     float* scores = kv.w ? lse + (size_t)b.n_seqs * n_q : nullptr;
-    const hipError_t e = attn8_generic(dt, q, q_stride, out, n_q, n_kv, d, b, kv, scores, lse, s);
+    hipError_t e = hipSuccess;
+    if (dt == F32 || force_generic) {
+        e = attn8_generic(dt, q, q_stride, out, n_q, n_kv, d, b, kv, scores, lse, s);
+    } else {
+        if (b.wk.n_items <= 0 || (long long)b.wk.n_items * n_kv * ((n_q / n_kv + 15) / 16) > 0x7fffffffll) return hipErrorInvalidValue;
+        if (d == 64) launch_decode<64>(q, q_stride, out, n_q, n_kv, b, kv, scratch, scores, lse, s);
+        else launch_decode<128>(q, q_stride, out, n_q, n_kv, b, kv, scratch, scores, lse, s);
+        e = hipGetLastError();
+    }
     if (e != hipSuccess || !kv.w) return e;
     attn8_weights_kernel<<<dim3((unsigned)(((long long)b.max_seen * n_kv + 255) / 256), b.n_seqs), 256, 0, s>>>(scores, lse, n_q, n_kv, b, kv.w);
     return hipGetLastError();
