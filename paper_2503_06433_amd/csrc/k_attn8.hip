@@ -112,14 +112,6 @@ static hipError_t attn8_generic(int dt, const void* q, int64_t q_stride, void* o
     return hipGetLastError();
 }
 
-hipError_t attn8_prefill(int dt, const void* q, int64_t q_stride, void* out, int n_q, int n_kv, int d, const Kv8Batch& b,
-                         const Kv8Layer& kv, bool force_generic, hipStream_t s) {
-    if (b.T <= 0 || b.n_seqs <= 0) return hipSuccess;
-    if (!attn8_fits(n_q, n_kv, d, b, q, q_stride, dt)) return hipErrorInvalidValue;
-    (void)force_generic;
-    return attn8_generic(dt, q, q_stride, out, n_q, n_kv, d, b, kv, nullptr, nullptr, s);
-}
-
 // ---------------------------------------------------------------- operands of the matrix cores
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
 union Frag8 {
@@ -438,6 +430,318 @@ static void launch_decode(const void* q, int64_t q_stride, void* out, int n_q, i
     const auto kernel = scores ? attn8_decode_kernel<D, true> : attn8_decode_kernel<D, false>;
     kernel<<<grid, 64, 0, s>>>((const bf16_t*)q, q_stride, n_q, n_kv, n_ct, b, kv, scratch, scores, sl2);
     attn8_merge_kernel<D, 1024 / D><<<dim3((n_q * D + 1023) / 1024, b.n_seqs), 256, 0, s>>>(scratch, (bf16_t*)out, n_q, b, lse);
+}
+
+// ---------------------------------------------------------------- prompts
+// A block of 8 waves takes 256 rows of one (sequence, kv head) at a time; a row is a query of one of the head's G query heads, the
+// heads of a token side by side, so that a few tokens of many heads fill a block like many tokens of one.  64 tokens (4 pages) at a
+// time come to LDS as numbers of the 16-bit type: every thread widens 16 bytes of K and 16 of V, once for all eight waves (each
+// wave widening its own operands would cost 1.5 times the vector operations of the softmax).  The whole numbers stay as they are: K's
+// step goes into the exponent's factor, V's into the weight (v_step).  Two stages: while one is multiplied, the next is
+// widened from registers and the one behind it requested.
+// K rows are stored with their 16-byte pieces swapped by the row number, V rows (16 tokens of an element) with their halves swapped
+// in rows 8 - 15 of 16: reads and writes of 16 lanes fall on all banks.
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
+
+__device__ __forceinline__ float max_of_halves(float x) {
+    const unsigned u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float lane_value(float x, int lane) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
+}
+
+// The reference of a row's exponents follows the largest only when that has grown by more than LAG: the largest weight is 2^TOP_ROW
+// to 2^(TOP_ROW + LAG) (half: 2^15, see TOP_EXP).
+constexpr float LAG = TOP_EXP > 0.f ? 4.f : 8.f;
+constexpr float TOP_ROW = TOP_EXP > 0.f ? 11.f : 0.f;
+
+template <int D> constexpr int prefill_stage = 2 * 64 * D * 2;
+
+template <int D>
+__global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __restrict__ q, int64_t q_stride, bf16_t* __restrict__ out, int n_q,
+                                                            int n_kv, Kv8Batch b, Kv8Layer kv, float scale_log2e) {
+    constexpr int KS = D / 16, DT = D / 32, ROW = 2 * D, KBYTES = 64 * ROW, STAGE = prefill_stage<D>;
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    const int G = n_q / n_kv;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lq = lane & 31, g2 = lane >> 5;
+    // what a thread widens: of a tile's page pg_w one piece of a K row and one row of V; heads of 64: half of the waves each
+    const int pg_w = D == 128 ? wave >> 1 : wave & 3;
+    const bool does_k = D == 128 || wave < 4, does_v = D == 128 || wave >= 4;
+    const int unit = D == 128 ? threadIdx.x & 127 : lane;                // within the page
+    const int k_tok = unit / (D / 16), k_piece = unit % (D / 16);
+    const int k_row = pg_w * 16 + k_tok;
+    const int k_swap = D == 128 ? k_row & 15 : (k_row >> 1) & 7;
+    const int r_swap = D == 128 ? lq & 15 : (lq >> 1) & 7;
+
+    for (int pj = 0;; ++pj) {
+        const int32_t* rec = b.pf_items + ((size_t)blockIdx.x * b.pf_stride + pj) * 8;
+        const int sq = __builtin_amdgcn_readfirstlane(rec[0]);
+        if (sq < 0) break;                                               // end of the list: the whole block leaves
+        const int g = __builtin_amdgcn_readfirstlane(rec[1]), row0 = __builtin_amdgcn_readfirstlane(rec[2]);
+        const int q_begin = __builtin_amdgcn_readfirstlane(rec[3]), rows = __builtin_amdgcn_readfirstlane(rec[4]) * G;
+        const int before = __builtin_amdgcn_readfirstlane(rec[5]), end = __builtin_amdgcn_readfirstlane(rec[6]);
+        const int full = end / 16;
+        const int wrow = row0 + wave * 32, row = wrow + lq;
+        const bool valid = row < rows, active = wrow < rows;
+        const int qi = (valid ? row : row0) / G, head = g * G + (valid ? row : row0) % G;
+        const int p = before + qi;
+        const int wave_first = before + wrow / G, wave_last = before + (wrow + 31 < rows ? wrow + 31 : rows - 1) / G;
+        const int blk_last = before + (row0 + 255 < rows ? row0 + 255 : rows - 1) / G;
+        const int n_pages = blk_last / 16 + 1, n_tiles = (n_pages + 3) / 4;
+        const int32_t* pt = b.page_tables + (size_t)sq * b.pt_stride;
+        const bf16_t* ko = (const bf16_t*)kv.open + ((size_t)b.slot[sq] * 2 * n_kv + g) * 16 * D;
+        const bf16_t* vo = ko + (size_t)n_kv * 16 * D;
+
+        half8_t qf[KS];
+        {
+            const bf16_t* qp = q + (int64_t)(q_begin + qi) * q_stride + (size_t)head * D + g2 * 8;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const half8_t*>(qp + ks * 16);
+        }
+        f32x16_t o[DT];
+#pragma unroll
+        for (int u = 0; u < DT; ++u)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[u][v] = 0.f;
+        float r = -INFINITY, l = 0.f;
+
+        // lane i holds what belongs to page i % 4 of a tile
+        struct Raw { vec16 k, v; float2 amax; };
+        auto load_ids = [&](int tile) {
+            const int j = tile * 4 + (lane & 3);
+            return pt[j < n_pages ? j : n_pages - 1];
+        };
+        auto load_raw = [&](int ids, Raw& w) {
+            const size_t page = ((size_t)__builtin_amdgcn_readlane(ids, pg_w) * n_kv + g) * 16 * D;
+            if (does_k) w.k = *reinterpret_cast<const vec16*>(kv.k + page + unit * 16);
+            if (does_v) w.v = *reinterpret_cast<const vec16*>(kv.v + page + unit * 16);
+            w.amax = *reinterpret_cast<const float2*>(kv.amax + ((size_t)ids * n_kv + g) * 2);
+        };
+        struct Steps { float ks, lv, inv; };                             // of page lane % 4
+        // LDS image of a tile; returns the steps of its pages
+        auto store = [&](int tile, const Raw& w) {
+            uint8_t* st = smem + (tile & 1) * STAGE;
+            uint8_t* kd = st + k_row * ROW;
+            uint8_t* vd = st + KBYTES + pg_w * (D * 32) + unit * 32;
+            const int vswap = (unit >> 3 & 1) * 16;
+            Steps s;
+            s.ks = w.amax.x / 127.f * scale_log2e;
+            s.ks = s.ks < 1e-37f ? 1e-37f : s.ks;                         // a block of zeros: any step, but no infinity times zero
+            v_step(w.amax.y, s.lv, s.inv);
+            if (tile * 4 + pg_w != full || full >= n_pages) {
+                if (does_k) {
+                    *reinterpret_cast<vec16*>(kd + ((2 * k_piece) ^ k_swap) * 16) = widen8(w.k.w[0], w.k.w[1]).q;
+                    *reinterpret_cast<vec16*>(kd + ((2 * k_piece + 1) ^ k_swap) * 16) = widen8(w.k.w[2], w.k.w[3]).q;
+                }
+                if (does_v) {
+                    *reinterpret_cast<vec16*>(vd + vswap) = widen8(w.v.w[0], w.v.w[2]).q;
+                    *reinterpret_cast<vec16*>(vd + (16 - vswap)) = widen8(w.v.w[1], w.v.w[3]).q;
+                }
+            }
+            return s;
+        };
+        // The open block's page of a tile: the model's type as it is, V times a power of two that brings it below 128 and without values
+        // that are not finite; tokens that have such are marked, their weight is to be NaN.
+        int bad = 0;
+        auto store_open = [&](int tile, Steps& s) {
+            const int cnt = end - full * 16;
+            float big = 0.f;
+            int mark = 0;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {                           // all of V by every wave: all need its step
+                const int at = (i * 64 + lane) * 8, tok = at / D;
+                if (tok < cnt) {
+                    float x[8];
+                    unpack16<bf16_t>(*reinterpret_cast<const vec16*>(vo + at), x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool fin = fabsf(x[e]) < INFINITY;
+                        big = fmaxf(big, fin ? fabsf(x[e]) : 0.f);
+                        mark |= fin ? 0 : 1 << tok;
+                    }
+                }
+            }
+            big = wave_max(big);
+#pragma unroll
+            for (int i = 32; i > 0; i >>= 1) mark |= __shfl_xor(mark, i, 64);
+            bad = mark;
+            int e = big > 0.f ? (int)(__float_as_uint(big) >> 23) - 127 - 6 : (int)LV_ZERO;
+            e = e < (int)LV_MIN ? (int)LV_MIN : e;
+            if ((lane & 3) == (full & 3)) s = Steps{scale_log2e, (float)e, exp2_fast((float)-e)};
+            if ((full & 3) != pg_w) return;
+            uint8_t* st = smem + (tile & 1) * STAGE;
+            uint8_t* kd = st + k_row * ROW;
+            uint8_t* vd = st + KBYTES + pg_w * (D * 32) + unit * 32;
+            const int vswap = (unit >> 3 & 1) * 16;
+            if (does_k) {
+                const vec16* kr = reinterpret_cast<const vec16*>(ko + k_tok * D + k_piece * 16);
+                *reinterpret_cast<vec16*>(kd + ((2 * k_piece) ^ k_swap) * 16) = kr[0];
+                *reinterpret_cast<vec16*>(kd + ((2 * k_piece + 1) ^ k_swap) * 16) = kr[1];
+            }
+            if (does_v) {
+                const float down = exp2_fast((float)-e);
+                float x[16];
+#pragma unroll
+                for (int t = 0; t < 16; ++t) {
+                    x[t] = t < cnt ? bf2f(vo[t * D + unit]) : 0.f;
+                    x[t] = fabsf(x[t]) < INFINITY ? x[t] * down : 0.f;
+                }
+                Frag8 lo, hi;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {                            // tokens 0 - 3, 8 - 11 and 4 - 7, 12 - 15
+                    lo.w[2 * i] = pack_bf16x2(x[8 * i], x[8 * i + 1]);
+                    lo.w[2 * i + 1] = pack_bf16x2(x[8 * i + 2], x[8 * i + 3]);
+                    hi.w[2 * i] = pack_bf16x2(x[8 * i + 4], x[8 * i + 5]);
+                    hi.w[2 * i + 1] = pack_bf16x2(x[8 * i + 6], x[8 * i + 7]);
+                }
+                *reinterpret_cast<vec16*>(vd + vswap) = lo.q;
+                *reinterpret_cast<vec16*>(vd + (16 - vswap)) = hi.q;
+            }
+        };
+
+        // 32 tokens of scores (pages 2 h and 2 h + 1 of the tile) become weights.  `hidden`: some of them are not to be seen by every row.
+        auto softmax = [&](f32x16_t& s, const Steps& st, int h, int t0, bool hidden, Frag8& pA, Frag8& pB) {
+            const float ksA = lane_value(st.ks, 2 * h), ksB = lane_value(st.ks, 2 * h + 1);
+            const float lvA = lane_value(st.lv, 2 * h), lvB = lane_value(st.lv, 2 * h + 1);
+            float mA = s[0], mB = s[8];
+#pragma unroll
+            for (int v = 1; v < 8; ++v) {
+                mA = fmaxf(mA, s[v]);
+                mB = fmaxf(mB, s[8 + v]);
+            }
+            const float top = max_of_halves(fmaxf(fmaf(mA, ksA, lvA), fmaf(mB, ksB, lvB))) - TOP_ROW;
+            const bool moved = top - r > LAG;                            // also in the first step (r = -infinity)
+            const float alpha = moved ? exp2_fast(r - top) : 1.f;
+            r = moved ? top : r;
+            const float offA = lvA - r, offB = lvB - r;
+            float sumA = 0.f, sumB = 0.f;
+#pragma unroll
+            for (int v = 0; v < 8; ++v) {
+                s[v] = exp2_fast(fmaf(s[v], ksA, offA));
+                s[8 + v] = exp2_fast(fmaf(s[8 + v], ksB, offB));
+            }
+            if (hidden) {                                                // the steps of a block that is not seen may not be numbers
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int t = t0 + 8 * (v >> 2) + 4 * g2 + (v & 3);
+                    s[v] = t <= p ? s[v] : 0.f;
+                    if (bad && t >= full * 16 && t <= p && (bad >> (t - full * 16) & 1)) s[v] = __uint_as_float(0x7fc00000u);
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < 8; ++v) {
+                sumA += s[v];
+                sumB += s[8 + v];
+            }
+            const float a = sumA * lane_value(st.inv, 2 * h), c = sumB * lane_value(st.inv, 2 * h + 1);
+            l = l * alpha + (hidden && t0 > p ? 0.f : a) + (hidden && t0 + 16 > p ? 0.f : c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                pA.w[i] = pack_bf16x2(s[2 * i], s[2 * i + 1]);
+                pB.w[i] = pack_bf16x2(s[8 + 2 * i], s[8 + 2 * i + 1]);
+            }
+            return alpha;
+        };
+        auto mask = [&](f32x16_t& s, int t0) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[v] = t0 + 8 * (v >> 2) + 4 * g2 + (v & 3) <= p ? s[v] : -INFINITY;
+        };
+        auto rescale = [&](float alpha) {
+            if (__any(alpha != 1.f)) {
+#pragma unroll
+                for (int u = 0; u < DT; ++u)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) o[u][v] *= alpha;
+            }
+        };
+        auto publish = [] {                                              // what this wave wrote is there before the others are let on
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+
+        int ids = load_ids(0);
+        Raw raw;
+        load_raw(ids, raw);
+        ids = load_ids(1);
+        Steps cur = store(0, raw), nxt = cur;
+        if (full < 4 && full < n_pages) store_open(0, cur);
+        load_raw(ids, raw);
+        ids = load_ids(2);
+        publish();
+        for (int it = 0; it < n_tiles; ++it) {
+            if (it + 1 < n_tiles) {
+                nxt = store(it + 1, raw);
+                if (full >> 2 == it + 1 && full < n_pages) store_open(it + 1, nxt);
+                load_raw(ids, raw);
+                ids = load_ids(it + 3);
+            }
+            if (active && it * 64 <= wave_last) {
+                const uint8_t* st = smem + (it & 1) * STAGE;
+                const bool diag = it * 64 + 63 > wave_first;
+                const uint8_t* kp = st + lq * ROW;
+                const uint8_t* vp = st + KBYTES + lq * 32 + (g2 ^ (lq >> 3 & 1)) * 16;
+                f32x16_t s0, s1;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s0[v] = s1[v] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+                    s0 = SS_MFMA_32x32x16(*reinterpret_cast<const half8_t*>(kp + (((ks * 2 + g2) ^ r_swap) << 4)), qf[ks], s0, 0, 0, 0);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+                    s1 = SS_MFMA_32x32x16(*reinterpret_cast<const half8_t*>(kp + 32 * ROW + (((ks * 2 + g2) ^ r_swap) << 4)), qf[ks], s1, 0, 0, 0);
+                Frag8 pA, pB;
+                if (diag) mask(s0, it * 64);
+                rescale(softmax(s0, cur, 0, it * 64, diag, pA, pB));
+#pragma unroll
+                for (int u = 0; u < DT; ++u) {
+                    o[u] = SS_MFMA_32x32x16(*reinterpret_cast<const half8_t*>(vp + u * 1024), pA.v, o[u], 0, 0, 0);
+                    o[u] = SS_MFMA_32x32x16(*reinterpret_cast<const half8_t*>(vp + D * 32 + u * 1024), pB.v, o[u], 0, 0, 0);
+                }
+                if (diag) mask(s1, it * 64 + 32);
+                rescale(softmax(s1, cur, 1, it * 64 + 32, diag, pA, pB));
+#pragma unroll
+                for (int u = 0; u < DT; ++u) {
+                    o[u] = SS_MFMA_32x32x16(*reinterpret_cast<const half8_t*>(vp + 2 * D * 32 + u * 1024), pA.v, o[u], 0, 0, 0);
+                    o[u] = SS_MFMA_32x32x16(*reinterpret_cast<const half8_t*>(vp + 3 * D * 32 + u * 1024), pB.v, o[u], 0, 0, 0);
+                }
+            }
+            cur = nxt;
+            publish();
+        }
+        l += __shfl_xor(l, 32, 64);
+        if (valid) {
+            const float inv = 1.f / l;
+            bf16_t* op = out + ((size_t)(q_begin + qi) * n_q + head) * D;
+#pragma unroll
+            for (int u = 0; u < DT; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<uint2*>(op + u * 32 + 8 * j + 4 * g2) =
+                        make_uint2(pack_bf16x2(o[u][4 * j] * inv, o[u][4 * j + 1] * inv), pack_bf16x2(o[u][4 * j + 2] * inv, o[u][4 * j + 3] * inv));
+        }
+    }
+}
+
+template <int D>
+static hipError_t launch_prefill(const void* q, int64_t q_stride, void* out, int n_q, int n_kv, const Kv8Batch& b, const Kv8Layer& kv, hipStream_t s) {
+    constexpr int LDS = 2 * prefill_stage<D>;
+    const float sl2 = 1.4426950408889634f / sqrtf((float)D);
+    attn8_prefill_kernel<D><<<(unsigned)b.pf_blocks, 512, LDS, s>>>((const bf16_t*)q, q_stride, (bf16_t*)out, n_q, n_kv, b, kv, sl2);
+    return hipGetLastError();
+}
+
+hipError_t attn8_prefill(int dt, const void* q, int64_t q_stride, void* out, int n_q, int n_kv, int d, const Kv8Batch& b,
+                         const Kv8Layer& kv, bool force_generic, hipStream_t s) {
+    if (b.T <= 0 || b.n_seqs <= 0) return hipSuccess;
+    if (!attn8_fits(n_q, n_kv, d, b, q, q_stride, dt)) return hipErrorInvalidValue;
+    if (dt == F32 || force_generic) return attn8_generic(dt, q, q_stride, out, n_q, n_kv, d, b, kv, nullptr, nullptr, s);
+    if (!b.pf_items || b.pf_blocks <= 0) return hipErrorInvalidValue;
+    return d == 64 ? launch_prefill<64>(q, q_stride, out, n_q, n_kv, b, kv, s) : launch_prefill<128>(q, q_stride, out, n_q, n_kv, b, kv, s);
 }
 
 // ---------------------------------------------------------------- accumulated weights

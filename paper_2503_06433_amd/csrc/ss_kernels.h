@@ -137,6 +137,9 @@ struct Kv8Batch {
     const int32_t* unit_pos0;
     const int32_t* unit_cnt;
     int n_units;
+    // work lists of prompts: block b walks the records pf_items[(b * pf_stride + j) * 8 .. +7] = (sequence, kv head, first row of a block of
+    // 256, first batch token of the sequence, its new tokens, before, end, 0) up to a sequence of -1; row r is query head r % G of
+    // the kv head's G, token r / G
     const int32_t* pf_items;
     int pf_stride, pf_blocks;
     DecodeWork wk;               // pages include the open block's

@@ -670,70 +670,6 @@ static int decode_item_pages(int64_t total_pages, int n_kv_local) {
     return (int)(n & ~1);
 }
 
-// Prefill attention work lists.  An item is (sequence, q head, block of 256 queries); its cost is the
-// number of 64-token tiles it visits plus a fixed part.  The blocks of the kernel (one per compute unit)
-// are dealt to the 8 XCDs round-robin by their index, so the items of one (sequence, kv head) -- which
-// read the same K and V pages -- all go to blocks of one residue modulo 8 and find those pages in one
-// L2.  Within a residue the items are taken sequence by sequence (longest first), kv head by kv head, last
-// query block first, and each goes to the block with the least work so far: the items of one (sequence,
-// kv head) then start at about the same time on different blocks and share the pages while they are in
-// the L2 (taking all items heaviest first balances 2 % better and reads twice as much from beyond L2).
-void prefill_items(ss_ctx* c, Shard* s, int n, const int32_t* q_lens, const int32_t* kv_before, std::vector<int32_t>* items,
-                   int* stride_out, int* blocks_out) {
-    struct PfItem { int32_t sq, a, qb, cost, len; };
-    const int G = s->nq_l / s->nkv_l;
-    const int per_x = std::max(1, c->n_cus / 8);
-    std::vector<std::vector<PfItem>> by_x(8);
-    for (int i = 0; i < n; ++i) {
-        const int nqb_i = (q_lens[i] + 255) / 256;
-        for (int g = 0; g < s->nkv_l; ++g) {
-            const int x = (int)(((int64_t)i * s->nkv_l + g) % 8);
-            for (int jg = 0; jg < G; ++jg)
-                for (int qb = 0; qb < nqb_i; ++qb) {
-                    const int last = kv_before[i] + std::min(qb * 256 + 255, q_lens[i] - 1);
-                    by_x[x].push_back({i, g * G + jg, qb, last / 64 + 1 + 2, kv_before[i] + q_lens[i]});
-                }
-        }
-    }
-    std::vector<std::vector<PfItem>> lists((size_t)8 * per_x);
-    for (int x = 0; x < 8; ++x) {
-        std::stable_sort(by_x[x].begin(), by_x[x].end(), [G](const PfItem& p, const PfItem& q) {
-            if (p.len != q.len) return p.len > q.len;
-            if (p.sq != q.sq) return p.sq < q.sq;
-            if (p.a / G != q.a / G) return p.a / G < q.a / G;
-            if (p.qb != q.qb) return p.qb > q.qb;
-            return p.a < q.a;
-        });
-        std::priority_queue<std::pair<int64_t, int>, std::vector<std::pair<int64_t, int>>, std::greater<std::pair<int64_t, int>>> load;
-        for (int k = 0; k < per_x; ++k) load.push({0, k});
-        for (const PfItem& it : by_x[x]) {
-            auto top = load.top();
-            load.pop();
-            lists[(size_t)top.second * 8 + x].push_back(it);
-            load.push({top.first + it.cost, top.second});
-        }
-    }
-    const int pf_blocks = *blocks_out = 8 * per_x;
-    size_t longest = 0;
-    for (const auto& l : lists) longest = std::max(longest, l.size());
-    const int pf_stride = *stride_out = (int)longest + 1;
-    // one 32-byte record per item, everything the block needs to start on it: sequence (-1 ends the
-    // list), q head, first query of the block, first token of the sequence in the batch, its number of
-    // new tokens, its number of cached tokens
-    std::vector<int32_t>& pf_items = *items;
-    pf_items.assign((size_t)pf_blocks * pf_stride * 8, -1);
-    int t0 = 0;
-    std::vector<int> q_begin(n);
-    for (int i = 0; i < n; ++i) { q_begin[i] = t0; t0 += q_lens[i]; }
-    for (int blk = 0; blk < pf_blocks; ++blk)
-        for (size_t j = 0; j < lists[blk].size(); ++j) {
-            int32_t* r = &pf_items[((size_t)blk * pf_stride + j) * 8];
-            const PfItem& it = lists[blk][j];
-            r[0] = it.sq; r[1] = it.a; r[2] = it.qb * 256; r[3] = q_begin[it.sq]; r[4] = q_lens[it.sq];
-            r[5] = kv_before[it.sq]; r[6] = 0; r[7] = 0;
-        }
-}
-
 // Builds (or reuses) the metadata of a batch.  Returns the slot, whose upload may still have to be made (`pending`).
 int prepare_batch(ss_ctx* c, Shard* s, const ss_batch* b, bool decode, MetaSlot** out) {
     const int n = b->n_seqs;
@@ -861,9 +797,69 @@ int prepare_batch(ss_ctx* c, Shard* s, const ss_batch* b, bool decode, MetaSlot*
     }
     const size_t n_units = unit_seq.size();
     const size_t n_items = item_seq.size();
+    // Prefill attention work lists.  An item is (sequence, q head, block of 256 queries); its cost is the
+    // number of 64-token tiles it visits plus a fixed part.  The blocks of the kernel (one per compute unit)
+    // are dealt to the 8 XCDs round-robin by their index, so the items of one (sequence, kv head) -- which
+    // read the same K and V pages -- all go to blocks of one residue modulo 8 and find those pages in one
+    // L2.  Within a residue the items are taken sequence by sequence (longest first), kv head by kv head, last
+    // query block first, and each goes to the block with the least work so far: the items of one (sequence,
+    // kv head) then start at about the same time on different blocks and share the pages while they are in
+    // the L2 (taking all items heaviest first balances 2 % better and reads twice as much from beyond L2).
     std::vector<int32_t> pf_items;
     int pf_stride = 0, pf_blocks = 0;
-    if (!decode && max_q > 64) prefill_items(c, s, n, b->q_lens, b->kv_lens_before, &pf_items, &pf_stride, &pf_blocks);
+    if (!decode && max_q > 64) {
+        struct PfItem { int32_t sq, a, qb, cost, len; };
+        const int G = s->nq_l / s->nkv_l;
+        const int per_x = std::max(1, c->n_cus / 8);
+        std::vector<std::vector<PfItem>> by_x(8);
+        for (int i = 0; i < n; ++i) {
+            const int nqb_i = (b->q_lens[i] + 255) / 256;
+            for (int g = 0; g < s->nkv_l; ++g) {
+                const int x = (int)(((int64_t)i * s->nkv_l + g) % 8);
+                for (int jg = 0; jg < G; ++jg)
+                    for (int qb = 0; qb < nqb_i; ++qb) {
+                        const int last = b->kv_lens_before[i] + std::min(qb * 256 + 255, b->q_lens[i] - 1);
+                        by_x[x].push_back({i, g * G + jg, qb, last / 64 + 1 + 2, b->kv_lens_before[i] + b->q_lens[i]});
+                    }
+            }
+        }
+        std::vector<std::vector<PfItem>> lists((size_t)8 * per_x);
+        for (int x = 0; x < 8; ++x) {
+            std::stable_sort(by_x[x].begin(), by_x[x].end(), [G](const PfItem& p, const PfItem& q) {
+                if (p.len != q.len) return p.len > q.len;
+                if (p.sq != q.sq) return p.sq < q.sq;
+                if (p.a / G != q.a / G) return p.a / G < q.a / G;
+                if (p.qb != q.qb) return p.qb > q.qb;
+                return p.a < q.a;
+            });
+            std::priority_queue<std::pair<int64_t, int>, std::vector<std::pair<int64_t, int>>, std::greater<std::pair<int64_t, int>>> load;
+            for (int k = 0; k < per_x; ++k) load.push({0, k});
+            for (const PfItem& it : by_x[x]) {
+                auto top = load.top();
+                load.pop();
+                lists[(size_t)top.second * 8 + x].push_back(it);
+                load.push({top.first + it.cost, top.second});
+            }
+        }
+        pf_blocks = 8 * per_x;
+        size_t longest = 0;
+        for (const auto& l : lists) longest = std::max(longest, l.size());
+        pf_stride = (int)longest + 1;
+        // one 32-byte record per item, everything the block needs to start on it: sequence (-1 ends the
+        // list), q head, first query of the block, first token of the sequence in the batch, its number of
+        // new tokens, its number of cached tokens
+        pf_items.assign((size_t)pf_blocks * pf_stride * 8, -1);
+        int t0 = 0;
+        std::vector<int> q_begin(n);
+        for (int i = 0; i < n; ++i) { q_begin[i] = t0; t0 += b->q_lens[i]; }
+        for (int blk = 0; blk < pf_blocks; ++blk)
+            for (size_t j = 0; j < lists[blk].size(); ++j) {
+                int32_t* r = &pf_items[((size_t)blk * pf_stride + j) * 8];
+                const PfItem& it = lists[blk][j];
+                r[0] = it.sq; r[1] = it.a; r[2] = it.qb * 256; r[3] = q_begin[it.sq]; r[4] = b->q_lens[it.sq];
+                r[5] = b->kv_lens_before[it.sq]; r[6] = 0; r[7] = 0;
+            }
+    }
     // launch order: longest items first, so that the last waves of the grid are the short ones
     std::vector<int32_t> item_order(n_items);
     for (size_t i = 0; i < n_items; ++i) item_order[i] = (int32_t)i;
@@ -1120,6 +1116,61 @@ struct Image {
     }
 };
 
+// Work lists of the prompts' attention over a cache in 8 bits.  An item is 256 rows of one (sequence, kv head), a row a query of one
+// of the head's query heads; it costs the tiles of 64 tokens it visits and a fixed part.  Blocks (one per compute
+// unit) are dealt to the XCDs by their index modulo 8.  The items are taken pair by pair, the longest sequence first, the last rows
+// first, and cut into eight shares of equal cost: those that read the same pages mostly share an L2, and few long
+// sequences still fill the chip.  Within a share each goes to the block with the least work so far.
+void prefill8_items(ss_ctx* c, Shard* s, int n, const std::vector<int32_t>& cu, const std::vector<int32_t>& before, const std::vector<int32_t>& end,
+                    std::vector<int32_t>* out, int* stride_out, int* blocks_out) {
+    struct Item { int32_t sq, g, row0, cost; };
+    const int G = s->nq_l / s->nkv_l, per_x = std::max(1, c->n_cus / 8);
+    std::vector<int32_t> order(n);
+    for (int i = 0; i < n; ++i) order[i] = i;
+    std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return before[x] + cu[x + 1] - cu[x] > before[y] + cu[y + 1] - cu[y]; });
+    std::vector<Item> items;
+    int64_t total = 0;
+    for (int i : order) {
+        const int64_t rows = (int64_t)(cu[i + 1] - cu[i]) * G;
+        for (int g = 0; g < s->nkv_l; ++g)
+            for (int64_t r0 = (rows - 1) / 256 * 256; r0 >= 0; r0 -= 256) {
+                const int last = before[i] + (int)(std::min(r0 + 255, rows - 1) / G);
+                items.push_back({i, g, (int32_t)r0, last / 64 + 3});
+                total += items.back().cost;
+            }
+    }
+    std::vector<std::vector<Item>> lists((size_t)8 * per_x);
+    typedef std::pair<int64_t, int> Load;
+    std::priority_queue<Load, std::vector<Load>, std::greater<Load>> load;
+    int x = -1;
+    int64_t done = 0;
+    for (const Item& it : items) {
+        const int to = (int)std::min<int64_t>(7, (done + it.cost / 2) * 8 / total);
+        if (to != x) {
+            x = to;
+            load = {};
+            for (int k = 0; k < per_x; ++k) load.push({0, k});
+        }
+        const Load top = load.top();
+        load.pop();
+        lists[(size_t)top.second * 8 + x].push_back(it);
+        load.push({top.first + it.cost, top.second});
+        done += it.cost;
+    }
+    size_t longest = 0;
+    for (const auto& l : lists) longest = std::max(longest, l.size());
+    const int stride = *stride_out = (int)longest + 1;
+    *blocks_out = 8 * per_x;
+    out->assign((size_t)lists.size() * stride * 8, -1);
+    for (size_t blk = 0; blk < lists.size(); ++blk)
+        for (size_t j = 0; j < lists[blk].size(); ++j) {
+            const Item& it = lists[blk][j];
+            int32_t* r = &(*out)[(blk * stride + j) * 8];
+            r[0] = it.sq; r[1] = it.g; r[2] = it.row0; r[3] = cu[it.sq]; r[4] = cu[it.sq + 1] - cu[it.sq];
+            r[5] = before[it.sq]; r[6] = end[it.sq]; r[7] = 0;
+        }
+}
+
 // Checks a batch over a cache in 8 bits, takes the pages of what it brings, builds (or finds) its metadata.  Nothing is changed unless
 // everything fits.
 int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool write, Meta8Slot** out) {
@@ -1172,7 +1223,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
         if (!s->seqs.count(b->seq_ids[i]))
             for (int j = 0; j < i; ++j)
                 if (b->seq_ids[j] == b->seq_ids[i]) return fail(c, SS_EINVAL, "sequence %lld is listed twice", (long long)b->seq_ids[i]);
-    if (T > (1 << 30)) return fail(c, SS_EINVAL, "batch too large");
+    if (T > (1 << 30) || (int64_t)max_q * (s->nq_l / s->nkv_l) > (1 << 30)) return fail(c, SS_EINVAL, "batch too large");
     if (decode && s->kv8_weights && seen > INT32_MAX) return fail(c, SS_EINVAL, "batch too large: it sees %lld tokens", (long long)seen);
     if (more > s->free_pages.size())
         return fail(c, SS_ENOMEM, "page pool exhausted: the batch needs %zu more pages, %zu free", more, s->free_pages.size());
@@ -1245,7 +1296,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
     }
     std::vector<int32_t> pf;
     int pf_stride = 0, pf_blocks = 0;
-    if (!decode && max_q > 64) prefill_items(c, s, n, b->q_lens, before.data(), &pf, &pf_stride, &pf_blocks);
+    if (!decode && c->dt != SS_F32) prefill8_items(c, s, n, cu, before, end, &pf, &pf_stride, &pf_blocks);
     Image im;
     const size_t o_cu = im.add(cu), o_before = im.add(before), o_end = im.add(end), o_slot = im.add(slot), o_pos = im.add(pos),
                  o_tok = im.add(tok_off), o_pt = im.add(pt), o_us = im.add(unit_seq), o_ut = im.add(unit_tok0), o_up = im.add(unit_pos0),
