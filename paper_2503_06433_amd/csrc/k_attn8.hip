@@ -2,6 +2,8 @@
 //
 // What is attended to is what the cache holds: full blocks stand for q * (A / 127), the block that is open at the end of a sequence
 // is read in the model's type.  Scores are kept in units of log 2.
+#include <type_traits>
+
 #include "ss_device.h"
 #include "ss_kernels.h"
 
@@ -154,8 +156,9 @@ constexpr float TOP_EXP = 14.f;
 #else
 constexpr float TOP_EXP = 0.f;
 #endif
+constexpr float ONE_127 = 1.f / 127.f;               // a step is formed with it: one more rounding of 2^-24, ten operations less than the quotient
 __device__ __forceinline__ void v_step(float amax, float& lv, float& inv) {
-    const float step = amax / 127.f, l = __builtin_amdgcn_logf(step);
+    const float l = __builtin_amdgcn_logf(amax * ONE_127);
     lv = amax == 0.f ? LV_ZERO : l < LV_MIN ? LV_MIN : l;
     inv = exp2_fast(-lv);
 }
@@ -245,7 +248,7 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
             __builtin_amdgcn_sched_barrier(0);
             load_k(nxt, fn);
             __builtin_amdgcn_sched_barrier(0);
-            const float ks = f.amax.x / 127.f * scale_log2e;
+            const float ks = f.amax.x * (ONE_127 * scale_log2e);
             float lv, inv;
             v_step(f.amax.y, lv, inv);
             const int pg = page0 + (j0 + g4) * stride;
@@ -474,8 +477,13 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
     const int unit = D == 128 ? threadIdx.x & 127 : lane;                // within the page
     const int k_tok = unit / (D / 16), k_piece = unit % (D / 16);
     const int k_row = pg_w * 16 + k_tok;
-    const int k_swap = D == 128 ? k_row & 15 : (k_row >> 1) & 7;
-    const int r_swap = D == 128 ? lq & 15 : (lq >> 1) & 7;
+    // byte offsets in a stage: where the thread writes its piece of K (the second half 16 bytes on, in the swapped order: ^ 16) and its row
+    // of V (likewise), where it reads the fragments of a score product (k-step ks: ^ 32 ks) and of V^T
+    const uint32_t k_write = k_row * ROW + (((2 * k_piece) ^ (D == 128 ? k_row & 15 : (k_row >> 1) & 7)) << 4);
+    const uint32_t v_write = KBYTES + pg_w * (D * 32) + unit * 32 + (unit >> 3 & 1) * 16;
+    const uint32_t k_read = lq * ROW + ((g2 ^ (D == 128 ? lq & 15 : (lq >> 1) & 7)) << 4);
+    const uint32_t v_read = KBYTES + lq * 32 + (g2 ^ (lq >> 3 & 1)) * 16;
+    auto lds = [&](uint32_t at) { return reinterpret_cast<vec16*>(smem + at); };
 
     for (int pj = 0;; ++pj) {
         const int32_t* rec = b.pf_items + ((size_t)blockIdx.x * b.pf_stride + pj) * 8;
@@ -517,34 +525,31 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
         };
         auto load_raw = [&](int ids, Raw& w) {
             const size_t page = ((size_t)__builtin_amdgcn_readlane(ids, pg_w) * n_kv + g) * 16 * D;
-            if (does_k) w.k = *reinterpret_cast<const vec16*>(kv.k + page + unit * 16);
-            if (does_v) w.v = *reinterpret_cast<const vec16*>(kv.v + page + unit * 16);
+            uint32_t at = unit * 16;                                     // 32 bits next to a scalar base, not two 64-bit addresses a lane
+            asm volatile("" : "+v"(at));
+            if (does_k) w.k = *reinterpret_cast<const vec16*>(kv.k + page + at);
+            if (does_v) w.v = *reinterpret_cast<const vec16*>(kv.v + page + at);
             w.amax = *reinterpret_cast<const float2*>(kv.amax + ((size_t)ids * n_kv + g) * 2);
         };
         struct Steps { float ks, lv, inv; };                             // of page lane % 4
         // LDS image of a tile; returns the steps of its pages
         auto store = [&](int tile, const Raw& w) {
-            uint8_t* st = smem + (tile & 1) * STAGE;
-            uint8_t* kd = st + k_row * ROW;
-            uint8_t* vd = st + KBYTES + pg_w * (D * 32) + unit * 32;
-            const int vswap = (unit >> 3 & 1) * 16;
+            const uint32_t st = (tile & 1) * STAGE;
             Steps s;
-            s.ks = w.amax.x / 127.f * scale_log2e;
+            s.ks = w.amax.x * (ONE_127 * scale_log2e);
             s.ks = s.ks < 1e-37f ? 1e-37f : s.ks;                         // a block of zeros: any step, but no infinity times zero
             v_step(w.amax.y, s.lv, s.inv);
-            if (tile * 4 + pg_w != full || full >= n_pages) {
-                if (does_k) {
-                    *reinterpret_cast<vec16*>(kd + ((2 * k_piece) ^ k_swap) * 16) = widen8(w.k.w[0], w.k.w[1]).q;
-                    *reinterpret_cast<vec16*>(kd + ((2 * k_piece + 1) ^ k_swap) * 16) = widen8(w.k.w[2], w.k.w[3]).q;
-                }
-                if (does_v) {
-                    *reinterpret_cast<vec16*>(vd + vswap) = widen8(w.v.w[0], w.v.w[2]).q;
-                    *reinterpret_cast<vec16*>(vd + (16 - vswap)) = widen8(w.v.w[1], w.v.w[3]).q;
-                }
+            if (does_k) {
+                *lds(st + k_write) = widen8(w.k.w[0], w.k.w[1]).q;
+                *lds((st + k_write) ^ 16) = widen8(w.k.w[2], w.k.w[3]).q;
+            }
+            if (does_v) {
+                *lds(st + v_write) = widen8(w.v.w[0], w.v.w[2]).q;
+                *lds((st + v_write) ^ 16) = widen8(w.v.w[1], w.v.w[3]).q;
             }
             return s;
         };
-        // The open block's page of a tile: the model's type as it is, V times a power of two that brings it below 128 and without values
+        // The open block's page of a tile, over what `store` brought there: the model's type as it is, V times a power of two that brings it below 128 and without values
         // that are not finite; tokens that have such are marked, their weight is to be NaN.
         int bad = 0;
         auto store_open = [&](int tile, Steps& s) {
@@ -573,14 +578,11 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
             e = e < (int)LV_MIN ? (int)LV_MIN : e;
             if ((lane & 3) == (full & 3)) s = Steps{scale_log2e, (float)e, exp2_fast((float)-e)};
             if ((full & 3) != pg_w) return;
-            uint8_t* st = smem + (tile & 1) * STAGE;
-            uint8_t* kd = st + k_row * ROW;
-            uint8_t* vd = st + KBYTES + pg_w * (D * 32) + unit * 32;
-            const int vswap = (unit >> 3 & 1) * 16;
+            const uint32_t st = (tile & 1) * STAGE;
             if (does_k) {
                 const vec16* kr = reinterpret_cast<const vec16*>(ko + k_tok * D + k_piece * 16);
-                *reinterpret_cast<vec16*>(kd + ((2 * k_piece) ^ k_swap) * 16) = kr[0];
-                *reinterpret_cast<vec16*>(kd + ((2 * k_piece + 1) ^ k_swap) * 16) = kr[1];
+                *lds(st + k_write) = kr[0];
+                *lds((st + k_write) ^ 16) = kr[1];
             }
             if (does_v) {
                 const float down = exp2_fast((float)-e);
@@ -598,13 +600,14 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
                     hi.w[2 * i] = pack_bf16x2(x[8 * i + 4], x[8 * i + 5]);
                     hi.w[2 * i + 1] = pack_bf16x2(x[8 * i + 6], x[8 * i + 7]);
                 }
-                *reinterpret_cast<vec16*>(vd + vswap) = lo.q;
-                *reinterpret_cast<vec16*>(vd + (16 - vswap)) = hi.q;
+                *lds(st + v_write) = lo.q;
+                *lds((st + v_write) ^ 16) = hi.q;
             }
         };
 
         // 32 tokens of scores (pages 2 h and 2 h + 1 of the tile) become weights.  `hidden`: some of them are not to be seen by every row.
-        auto softmax = [&](f32x16_t& s, const Steps& st, int h, int t0, bool hidden, Frag8& pA, Frag8& pB) {
+        auto softmax = [&](auto hidden_c, f32x16_t& s, const Steps& st, int h, int t0, Frag8& pA, Frag8& pB) {
+            constexpr bool hidden = decltype(hidden_c)::value;
             const float ksA = lane_value(st.ks, 2 * h), ksB = lane_value(st.ks, 2 * h + 1);
             const float lvA = lane_value(st.lv, 2 * h), lvB = lane_value(st.lv, 2 * h + 1);
             float mA = s[0], mB = s[8];
@@ -624,7 +627,7 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
                 s[v] = exp2_fast(fmaf(s[v], ksA, offA));
                 s[8 + v] = exp2_fast(fmaf(s[8 + v], ksB, offB));
             }
-            if (hidden) {                                                // the steps of a block that is not seen may not be numbers
+            if constexpr (hidden) {                                      // the steps of a block that is not seen may not be numbers
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int t = t0 + 8 * (v >> 2) + 4 * g2 + (v & 3);
@@ -644,6 +647,8 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
                 pA.w[i] = pack_bf16x2(s[2 * i], s[2 * i + 1]);
                 pB.w[i] = pack_bf16x2(s[8 + 2 * i], s[8 + 2 * i + 1]);
             }
+            // complete here, not wherever their first use is moved to
+            asm volatile("" : "+v"(pA.w[0]), "+v"(pA.w[1]), "+v"(pA.w[2]), "+v"(pA.w[3]), "+v"(pB.w[0]), "+v"(pB.w[1]), "+v"(pB.w[2]), "+v"(pB.w[3]));
             return alpha;
         };
         auto mask = [&](f32x16_t& s, int t0) {
@@ -651,7 +656,7 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
             for (int v = 0; v < 16; ++v) s[v] = t0 + 8 * (v >> 2) + 4 * g2 + (v & 3) <= p ? s[v] : -INFINITY;
         };
         auto rescale = [&](float alpha) {
-            if (__any(alpha != 1.f)) {
+            if (__builtin_expect(__any(alpha != 1.f), 0)) {              // said to be rare, so that the other path needs no copies of o
 #pragma unroll
                 for (int u = 0; u < DT; ++u)
 #pragma unroll
@@ -664,6 +669,34 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
             asm volatile("" ::: "memory");
         };
 
+        // One tile; the scores of its second half are asked for in front of the softmax of the first, so that products and vector
+        // operations can stand side by side.
+        auto tile = [&](auto hidden_c, int it, const Steps& st) {
+            constexpr bool hidden = decltype(hidden_c)::value;
+            const uint32_t kp = (it & 1) * STAGE + k_read, vp = (it & 1) * STAGE + v_read;
+            auto read_k = [&](int h, int ks) { return *reinterpret_cast<const half8_t*>(lds((kp ^ (ks * 32)) + h * 32 * ROW)); };
+            auto read_v = [&](int h, int i) { return *reinterpret_cast<const half8_t*>(lds(vp + (2 * h + (i & 1)) * D * 32 + (i >> 1) * 1024)); };
+            f32x16_t s0, s1;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s0[v] = s1[v] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s0 = SS_MFMA_32x32x16(read_k(0, ks), qf[ks], s0, 0, 0, 0);
+            if constexpr (hidden) mask(s0, it * 64);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s1 = SS_MFMA_32x32x16(read_k(1, ks), qf[ks], s1, 0, 0, 0);
+            Frag8 pA, pB;
+            float alpha = softmax(hidden_c, s0, st, 0, it * 64, pA, pB);
+            rescale(alpha);
+#pragma unroll
+            for (int i = 0; i < KS; ++i) o[i >> 1] = SS_MFMA_32x32x16(read_v(0, i), i & 1 ? pB.v : pA.v, o[i >> 1], 0, 0, 0);
+            if constexpr (hidden) mask(s1, it * 64 + 32);
+            Frag8 pC, pD;
+            alpha = softmax(hidden_c, s1, st, 1, it * 64 + 32, pC, pD);
+            rescale(alpha);
+#pragma unroll
+            for (int i = 0; i < KS; ++i) o[i >> 1] = SS_MFMA_32x32x16(read_v(1, i), i & 1 ? pD.v : pC.v, o[i >> 1], 0, 0, 0);
+        };
+
         int ids = load_ids(0);
         Raw raw;
         load_raw(ids, raw);
@@ -673,43 +706,24 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
         load_raw(ids, raw);
         ids = load_ids(2);
         publish();
-        for (int it = 0; it < n_tiles; ++it) {
-            if (it + 1 < n_tiles) {
-                nxt = store(it + 1, raw);
-                if (full >> 2 == it + 1 && full < n_pages) store_open(it + 1, nxt);
-                load_raw(ids, raw);
-                ids = load_ids(it + 3);
-            }
-            if (active && it * 64 <= wave_last) {
-                const uint8_t* st = smem + (it & 1) * STAGE;
-                const bool diag = it * 64 + 63 > wave_first;
-                const uint8_t* kp = st + lq * ROW;
-                const uint8_t* vp = st + KBYTES + lq * 32 + (g2 ^ (lq >> 3 & 1)) * 16;
-                f32x16_t s0, s1;
-#pragma unroll
-                for (int v = 0; v < 16; ++v) s0[v] = s1[v] = 0.f;
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    s0 = SS_MFMA_32x32x16(*reinterpret_cast<const half8_t*>(kp + (((ks * 2 + g2) ^ r_swap) << 4)), qf[ks], s0, 0, 0, 0);
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    s1 = SS_MFMA_32x32x16(*reinterpret_cast<const half8_t*>(kp + 32 * ROW + (((ks * 2 + g2) ^ r_swap) << 4)), qf[ks], s1, 0, 0, 0);
-                Frag8 pA, pB;
-                if (diag) mask(s0, it * 64);
-                rescale(softmax(s0, cur, 0, it * 64, diag, pA, pB));
-#pragma unroll
-                for (int u = 0; u < DT; ++u) {
-                    o[u] = SS_MFMA_32x32x16(*reinterpret_cast<const half8_t*>(vp + u * 1024), pA.v, o[u], 0, 0, 0);
-                    o[u] = SS_MFMA_32x32x16(*reinterpret_cast<const half8_t*>(vp + D * 32 + u * 1024), pB.v, o[u], 0, 0, 0);
-                }
-                if (diag) mask(s1, it * 64 + 32);
-                rescale(softmax(s1, cur, 1, it * 64 + 32, diag, pA, pB));
-#pragma unroll
-                for (int u = 0; u < DT; ++u) {
-                    o[u] = SS_MFMA_32x32x16(*reinterpret_cast<const half8_t*>(vp + 2 * D * 32 + u * 1024), pA.v, o[u], 0, 0, 0);
-                    o[u] = SS_MFMA_32x32x16(*reinterpret_cast<const half8_t*>(vp + 3 * D * 32 + u * 1024), pB.v, o[u], 0, 0, 0);
-                }
-            }
+        // Behind the last tile the last pages are brought once more, to a stage that nobody reads.
+        auto bring = [&](int it) {
+            nxt = store(it + 1, raw);
+            load_raw(ids, raw);
+            ids = load_ids(it + 3);
+            if (full >> 2 == it + 1 && full < n_pages) store_open(it + 1, nxt);
+        };
+        // first the tiles that every row of the wave sees all of
+        int it = 0;
+        for (; it < n_tiles && active && it * 64 + 63 <= wave_first; ++it) {
+            bring(it);
+            tile(std::false_type{}, it, cur);
+            cur = nxt;
+            publish();
+        }
+        for (; it < n_tiles; ++it) {
+            bring(it);
+            if (active && it * 64 <= wave_last) tile(std::true_type{}, it, cur);
             cur = nxt;
             publish();
         }
