@@ -442,8 +442,10 @@ static void launch_decode(const void* q, int64_t q_stride, void* out, int n_q, i
 // wave widening its own operands would cost 1.5 times the vector operations of the softmax).  The whole numbers stay as they are: K's
 // step goes into the exponent's factor, V's into the weight (v_step).  Two stages: while one is multiplied, the next is
 // widened from registers and the one behind it requested.
-// K rows are stored with their 16-byte pieces swapped by the row number, V rows (16 tokens of an element) with their halves swapped
-// in rows 8 - 15 of 16: reads and writes of 16 lanes fall on all banks.
+// Row r of a score product is token 4 (r / 8) + r % 4 of the first page of two (r % 8 < 4) or the second: accumulator v of a lane is
+// then token v of page 2 h + lane / 32, and a lane needs one K and one V step for its 16 scores.
+// K rows are stored with their 16-byte pieces swapped by token and page, V rows (16 tokens of an element) with their halves swapped in
+// rows 8 - 15 of 16: reads and writes of 16 lanes fall on all banks.
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
 
 __device__ __forceinline__ float max_of_halves(float x) {
@@ -451,8 +453,15 @@ __device__ __forceinline__ float max_of_halves(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float lane_value(float x, int lane) {
-    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
+// the value of the lane next to it (lanes 0 and 1, 2 and 3, ... swapped)
+__device__ __forceinline__ float neighbour(float x) {
+    return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0xb1, 0xf, 0xf, true));
+}
+// one instruction; fmaxf would first make its operands from the matrix cores canonical, one by one
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
 }
 
 // The reference of a row's exponents follows the largest only when that has grown by more than LAG: the largest weight is 2^TOP_ROW
@@ -476,13 +485,14 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
     const bool does_k = D == 128 || wave < 4, does_v = D == 128 || wave >= 4;
     const int unit = D == 128 ? threadIdx.x & 127 : lane;                // within the page
     const int k_tok = unit / (D / 16), k_piece = unit % (D / 16);
-    const int k_row = pg_w * 16 + k_tok;
+    auto k_swap = [](int page, int tok) { return D == 128 ? (tok & 7) | (page & 1) << 3 : (tok >> 1 & 3) | (page & 1) << 2; };
     // byte offsets in a stage: where the thread writes its piece of K (the second half 16 bytes on, in the swapped order: ^ 16) and its row
     // of V (likewise), where it reads the fragments of a score product (k-step ks: ^ 32 ks) and of V^T
-    const uint32_t k_write = k_row * ROW + (((2 * k_piece) ^ (D == 128 ? k_row & 15 : (k_row >> 1) & 7)) << 4);
+    const uint32_t k_write = (pg_w * 16 + k_tok) * ROW + (((2 * k_piece) ^ k_swap(pg_w, k_tok)) << 4);
     const uint32_t v_write = KBYTES + pg_w * (D * 32) + unit * 32 + (unit >> 3 & 1) * 16;
-    const uint32_t k_read = lq * ROW + ((g2 ^ (D == 128 ? lq & 15 : (lq >> 1) & 7)) << 4);
-    const uint32_t v_read = KBYTES + lq * 32 + (g2 ^ (lq >> 3 & 1)) * 16;
+    const int r_page = lq >> 2 & 1, r_tok = (lq >> 3) * 4 + (lq & 3);
+    const uint32_t k_read = (r_page * 16 + r_tok) * ROW + ((g2 ^ k_swap(r_page, r_tok)) << 4);
+    const uint32_t v_read = KBYTES + g2 * (D * 32) + lq * 32 + (lq >> 3 & 1) * 16;
     auto lds = [&](uint32_t at) { return reinterpret_cast<vec16*>(smem + at); };
 
     for (int pj = 0;; ++pj) {
@@ -517,21 +527,22 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
             for (int v = 0; v < 16; ++v) o[u][v] = 0.f;
         float r = -INFINITY, l = 0.f;
 
-        // lane i holds what belongs to page i % 4 of a tile
+        // a lane holds what belongs to page lane / 32 of a tile or, odd lanes, the second behind it
+        const int my_page = g2 + 2 * (lane & 1);
         struct Raw { vec16 k, v; float2 amax; };
         auto load_ids = [&](int tile) {
-            const int j = tile * 4 + (lane & 3);
+            const int j = tile * 4 + my_page;
             return pt[j < n_pages ? j : n_pages - 1];
         };
         auto load_raw = [&](int ids, Raw& w) {
-            const size_t page = ((size_t)__builtin_amdgcn_readlane(ids, pg_w) * n_kv + g) * 16 * D;
+            const size_t page = ((size_t)__builtin_amdgcn_readlane(ids, (pg_w & 1) * 32 + (pg_w >> 1)) * n_kv + g) * 16 * D;
             uint32_t at = unit * 16;                                     // 32 bits next to a scalar base, not two 64-bit addresses a lane
             asm volatile("" : "+v"(at));
             if (does_k) w.k = *reinterpret_cast<const vec16*>(kv.k + page + at);
             if (does_v) w.v = *reinterpret_cast<const vec16*>(kv.v + page + at);
             w.amax = *reinterpret_cast<const float2*>(kv.amax + ((size_t)ids * n_kv + g) * 2);
         };
-        struct Steps { float ks, lv, inv; };                             // of page lane % 4
+        struct Steps { float ks, lv, inv; };                             // of the lane's page
         // LDS image of a tile; returns the steps of its pages
         auto store = [&](int tile, const Raw& w) {
             const uint32_t st = (tile & 1) * STAGE;
@@ -544,8 +555,8 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
                 *lds((st + k_write) ^ 16) = widen8(w.k.w[2], w.k.w[3]).q;
             }
             if (does_v) {
-                *lds(st + v_write) = widen8(w.v.w[0], w.v.w[2]).q;
-                *lds((st + v_write) ^ 16) = widen8(w.v.w[1], w.v.w[3]).q;
+                *lds(st + v_write) = widen8(w.v.w[0], w.v.w[1]).q;
+                *lds((st + v_write) ^ 16) = widen8(w.v.w[2], w.v.w[3]).q;
             }
             return s;
         };
@@ -576,7 +587,7 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
             bad = mark;
             int e = big > 0.f ? (int)(__float_as_uint(big) >> 23) - 127 - 6 : (int)LV_ZERO;
             e = e < (int)LV_MIN ? (int)LV_MIN : e;
-            if ((lane & 3) == (full & 3)) s = Steps{scale_log2e, (float)e, exp2_fast((float)-e)};
+            if (my_page == (full & 3)) s = Steps{scale_log2e, (float)e, exp2_fast((float)-e)};
             if ((full & 3) != pg_w) return;
             const uint32_t st = (tile & 1) * STAGE;
             if (does_k) {
@@ -594,66 +605,50 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
                 }
                 Frag8 lo, hi;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {                            // tokens 0 - 3, 8 - 11 and 4 - 7, 12 - 15
-                    lo.w[2 * i] = pack_bf16x2(x[8 * i], x[8 * i + 1]);
-                    lo.w[2 * i + 1] = pack_bf16x2(x[8 * i + 2], x[8 * i + 3]);
-                    hi.w[2 * i] = pack_bf16x2(x[8 * i + 4], x[8 * i + 5]);
-                    hi.w[2 * i + 1] = pack_bf16x2(x[8 * i + 6], x[8 * i + 7]);
+                for (int i = 0; i < 4; ++i) {
+                    lo.w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+                    hi.w[i] = pack_bf16x2(x[8 + 2 * i], x[9 + 2 * i]);
                 }
                 *lds(st + v_write) = lo.q;
                 *lds((st + v_write) ^ 16) = hi.q;
             }
         };
 
-        // 32 tokens of scores (pages 2 h and 2 h + 1 of the tile) become weights.  `hidden`: some of them are not to be seen by every row.
-        auto softmax = [&](auto hidden_c, f32x16_t& s, const Steps& st, int h, int t0, Frag8& pA, Frag8& pB) {
+        // 32 tokens of scores, of the lane's page 16, become weights.  `hidden`: some of them are not to be seen by every row.
+        auto softmax = [&](auto hidden_c, f32x16_t& s, float ks, float lv, float inv, int t0, Frag8& pA, Frag8& pB) {
             constexpr bool hidden = decltype(hidden_c)::value;
-            const float ksA = lane_value(st.ks, 2 * h), ksB = lane_value(st.ks, 2 * h + 1);
-            const float lvA = lane_value(st.lv, 2 * h), lvB = lane_value(st.lv, 2 * h + 1);
-            float mA = s[0], mB = s[8];
+            if constexpr (hidden) {
 #pragma unroll
-            for (int v = 1; v < 8; ++v) {
-                mA = fmaxf(mA, s[v]);
-                mB = fmaxf(mB, s[8 + v]);
+                for (int v = 0; v < 16; ++v) s[v] = t0 + v <= p ? s[v] : -INFINITY;
             }
-            const float top = max_of_halves(fmaxf(fmaf(mA, ksA, lvA), fmaf(mB, ksB, lvB))) - TOP_ROW;
+            float m = max3(s[0], s[1], s[2]);
+#pragma unroll
+            for (int v = 3; v < 15; v += 2) m = max3(m, s[v], s[v + 1]);
+            const float top = max_of_halves(fmaf(fmaxf(m, s[15]), ks, lv)) - TOP_ROW;
             const bool moved = top - r > LAG;                            // also in the first step (r = -infinity)
             const float alpha = moved ? exp2_fast(r - top) : 1.f;
             r = moved ? top : r;
-            const float offA = lvA - r, offB = lvB - r;
-            float sumA = 0.f, sumB = 0.f;
+            const float off = lv - r;
+            float sum = 0.f;
 #pragma unroll
-            for (int v = 0; v < 8; ++v) {
-                s[v] = exp2_fast(fmaf(s[v], ksA, offA));
-                s[8 + v] = exp2_fast(fmaf(s[8 + v], ksB, offB));
-            }
-            if constexpr (hidden) {                                      // the steps of a block that is not seen may not be numbers
-#pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int t = t0 + 8 * (v >> 2) + 4 * g2 + (v & 3);
-                    s[v] = t <= p ? s[v] : 0.f;
-                    if (bad && t >= full * 16 && t <= p && (bad >> (t - full * 16) & 1)) s[v] = __uint_as_float(0x7fc00000u);
+            for (int v = 0; v < 16; ++v) {
+                s[v] = exp2_fast(fmaf(s[v], ks, off));
+                if constexpr (hidden) {                                  // the steps of a block that is not seen may not be numbers
+                    s[v] = t0 + v <= p ? s[v] : 0.f;
+                    if (bad && t0 + v >= full * 16 && t0 + v <= p && (bad >> (t0 + v - full * 16) & 1)) s[v] = __uint_as_float(0x7fc00000u);
                 }
+                sum += s[v];
             }
-#pragma unroll
-            for (int v = 0; v < 8; ++v) {
-                sumA += s[v];
-                sumB += s[8 + v];
-            }
-            const float a = sumA * lane_value(st.inv, 2 * h), c = sumB * lane_value(st.inv, 2 * h + 1);
-            l = l * alpha + (hidden && t0 > p ? 0.f : a) + (hidden && t0 + 16 > p ? 0.f : c);
+            sum *= inv;
+            l = l * alpha + (hidden && t0 > p ? 0.f : sum);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 pA.w[i] = pack_bf16x2(s[2 * i], s[2 * i + 1]);
-                pB.w[i] = pack_bf16x2(s[8 + 2 * i], s[8 + 2 * i + 1]);
+                pB.w[i] = pack_bf16x2(s[8 + 2 * i], s[9 + 2 * i]);
             }
             // complete here, not wherever their first use is moved to
             asm volatile("" : "+v"(pA.w[0]), "+v"(pA.w[1]), "+v"(pA.w[2]), "+v"(pA.w[3]), "+v"(pB.w[0]), "+v"(pB.w[1]), "+v"(pB.w[2]), "+v"(pB.w[3]));
             return alpha;
-        };
-        auto mask = [&](f32x16_t& s, int t0) {
-#pragma unroll
-            for (int v = 0; v < 16; ++v) s[v] = t0 + 8 * (v >> 2) + 4 * g2 + (v & 3) <= p ? s[v] : -INFINITY;
         };
         auto rescale = [&](float alpha) {
             if (__builtin_expect(__any(alpha != 1.f), 0)) {              // said to be rare, so that the other path needs no copies of o
@@ -675,23 +670,24 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
             constexpr bool hidden = decltype(hidden_c)::value;
             const uint32_t kp = (it & 1) * STAGE + k_read, vp = (it & 1) * STAGE + v_read;
             auto read_k = [&](int h, int ks) { return *reinterpret_cast<const half8_t*>(lds((kp ^ (ks * 32)) + h * 32 * ROW)); };
-            auto read_v = [&](int h, int i) { return *reinterpret_cast<const half8_t*>(lds(vp + (2 * h + (i & 1)) * D * 32 + (i >> 1) * 1024)); };
+            auto read_v = [&](int h, int i) { return *reinterpret_cast<const half8_t*>(lds((vp ^ (i & 1) * 16) + h * D * 64 + (i >> 1) * 1024)); };
+            const float ks_n = neighbour(st.ks), lv_n = neighbour(st.lv), inv_n = neighbour(st.inv);
+            const bool odd = lane & 1;
+            const int t0 = it * 64 + g2 * 16;
             f32x16_t s0, s1;
 #pragma unroll
             for (int v = 0; v < 16; ++v) s0[v] = s1[v] = 0.f;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) s0 = SS_MFMA_32x32x16(read_k(0, ks), qf[ks], s0, 0, 0, 0);
-            if constexpr (hidden) mask(s0, it * 64);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) s1 = SS_MFMA_32x32x16(read_k(1, ks), qf[ks], s1, 0, 0, 0);
             Frag8 pA, pB;
-            float alpha = softmax(hidden_c, s0, st, 0, it * 64, pA, pB);
+            float alpha = softmax(hidden_c, s0, odd ? ks_n : st.ks, odd ? lv_n : st.lv, odd ? inv_n : st.inv, t0, pA, pB);
             rescale(alpha);
 #pragma unroll
             for (int i = 0; i < KS; ++i) o[i >> 1] = SS_MFMA_32x32x16(read_v(0, i), i & 1 ? pB.v : pA.v, o[i >> 1], 0, 0, 0);
-            if constexpr (hidden) mask(s1, it * 64 + 32);
             Frag8 pC, pD;
-            alpha = softmax(hidden_c, s1, st, 1, it * 64 + 32, pC, pD);
+            alpha = softmax(hidden_c, s1, odd ? st.ks : ks_n, odd ? st.lv : lv_n, odd ? st.inv : inv_n, t0 + 32, pC, pD);
             rescale(alpha);
 #pragma unroll
             for (int i = 0; i < KS; ++i) o[i >> 1] = SS_MFMA_32x32x16(read_v(1, i), i & 1 ? pD.v : pC.v, o[i >> 1], 0, 0, 0);
