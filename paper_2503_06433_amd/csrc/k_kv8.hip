@@ -17,6 +17,23 @@ template <typename T> __device__ __forceinline__ int kv8_round(float v, float am
     if (sizeof(T) == 4 && fabsf(t - r) > 0.499f) return (int)rint((double)v * 127.0 / (double)amax);
     return (int)r;
 }
+// N of them: by the reciprocal (rc = 1 / amax), off from the quotient by at most 127 * 3 * 2^-24 < 2.3e-5; where that could decide, by the
+// division, which is ten times the instructions.
+template <typename T, int N>
+__device__ __forceinline__ void kv8_round_n(const float* v, float amax, float rc, int* q) {
+    constexpr float FAR = sizeof(T) == 4 ? 0.4989f : 0.4999f;
+    bool far = amax > 0.f && amax < INFINITY;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const float t = v[j] * 127.f * rc, r = rintf(t);
+        q[j] = (int)r;
+        far = far && fabsf(t - r) < FAR;
+    }
+    if (!far) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) q[j] = kv8_round<T>(v[j], amax);
+    }
+}
 __device__ __forceinline__ float kv8_step(float amax) { return amax / 127.f; }
 // a value that is not finite makes the block's magnitude NaN, and no other way round (fmaxf would drop a NaN)
 __device__ __forceinline__ float kv8_mag(float v) { const float a = fabsf(v); return a < INFINITY ? a : INFINITY; }
@@ -65,7 +82,7 @@ __device__ __forceinline__ void kv8_store_block(const Kv8Tile<T, D>& k, const Kv
         amax[0] = kv8_amax(mk);
         amax[1] = kv8_amax(mv);
     }
-    const float fk = kv8_fit(mk), fv = kv8_fit(mv), ak = mk * fk, av = mv * fv;
+    const float fk = kv8_fit(mk), fv = kv8_fit(mv), ak = mk * fk, av = mv * fv, rk = 1.f / ak, rv = 1.f / av;
     if (!Tile::idle(lane)) {
 #pragma unroll
         for (int p = 0; p < Tile::NP; ++p) {
@@ -74,17 +91,21 @@ __device__ __forceinline__ void kv8_store_block(const Kv8Tile<T, D>& k, const Kv
             for (int i = 0; i < 4; ++i) {
 #pragma unroll
                 for (int e = 0; e < Tile::EV; e += 4) {
+                    float x[4];
                     int q[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) q[j] = kv8_round<T>(k.x[i][p * Tile::EV + e + j] * fk, ak);
+                    for (int j = 0; j < 4; ++j) x[j] = k.x[i][p * Tile::EV + e + j] * fk;
+                    kv8_round_n<T, 4>(x, ak, rk, q);
                     *reinterpret_cast<uint32_t*>(kp + (4 * (lane >> 4) + i) * D + c + e) = kv8_pack4(q);
                 }
             }
 #pragma unroll
             for (int e = 0; e < Tile::EV; ++e) {
+                float x[4];
                 int q[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) q[i] = kv8_round<T>(v.x[i][p * Tile::EV + e] * fv, av);
+                for (int i = 0; i < 4; ++i) x[i] = v.x[i][p * Tile::EV + e] * fv;
+                kv8_round_n<T, 4>(x, av, rv, q);
                 lds[kv8_vword(c + e, lane >> 4)] = kv8_pack4(q);
             }
         }
@@ -359,7 +380,8 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
 // Which tokens stay.  A block per (head, layer, sequence).  The key of the last token that stays among the older ones is found digit
 // by digit (four histograms of 256), then one ordered pass lists the positions: all above that key, and of those
 // equal to it the first ones.
-constexpr int EV_T = 1024;
+// Keys are read from the cache once, to LDS, those behind the EV_KEYS first ones for every pass again.
+constexpr int EV_T = 1024, EV_KEYS = 36 * 1024;
 __global__ __launch_bounds__(EV_T) void kv8_select_kernel(const Kv8Layer* __restrict__ layers, int n_heads, Kv8Evict e, int32_t* __restrict__ lists) {
     __shared__ int hist[256], digit_s, left_s, eq_w[EV_T / 64], out_w[EV_T / 64];
     const int g = blockIdx.x, layer = blockIdx.y, sq = blockIdx.z;
@@ -373,7 +395,11 @@ __global__ __launch_bounds__(EV_T) void kv8_select_kernel(const Kv8Layer* __rest
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int i = tid; i < recent; i += EV_T) list[k + i] = n + i;
     if (k == 0) return;
-    auto key_at = [&](int t) { return evict_key(w[((size_t)pt[t >> 4] * n_heads + g) * 16 + (t & 15)]); };
+    extern __shared__ uint32_t keys[];
+    auto fetch = [&](int t) { return evict_key(w[((size_t)pt[t >> 4] * n_heads + g) * 16 + (t & 15)]); };
+    auto key_at = [&](int t) { return t < EV_KEYS ? keys[t] : fetch(t); };
+#pragma unroll 4
+    for (int t = tid; t < n && t < EV_KEYS; t += EV_T) keys[t] = fetch(t);
     uint32_t prefix = 0;
     int left = k;                         // how many of those with the prefix stay
     for (int shift = 24; shift >= 0; shift -= 8) {
@@ -384,11 +410,23 @@ __global__ __launch_bounds__(EV_T) void kv8_select_kernel(const Kv8Layer* __rest
             if (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[key >> shift & 255], 1);
         }
         __syncthreads();
-        if (tid == 0) {
-            int d = 255, rest = left;
-            while (hist[d] < rest) rest -= hist[d--];
-            digit_s = d;
-            left_s = rest;
+        if (wave == 0) {                  // lane l counts what lies above its digits 255 - 4 l .. 252 - 4 l; the digit where `left` is passed
+            int h[4], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += h[i] = hist[255 - 4 * lane - i];
+            int above = sum;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int x = __shfl_up(above, o, 64);
+                if (lane >= o) above += x;
+            }
+            above -= sum;
+            if (above < left && left <= above + sum) {
+                int i = 0, rest = left - above;
+                while (h[i] < rest) rest -= h[i++];
+                digit_s = 255 - 4 * lane - i;
+                left_s = rest;
+            }
         }
         __syncthreads();
         prefix |= (uint32_t)digit_s << shift;
@@ -424,20 +462,22 @@ __global__ __launch_bounds__(EV_T) void kv8_select_kernel(const Kv8Layer* __rest
     }
 }
 
-// Moves the kept tokens to the front, in place.  A block per (head, layer, sequence), a wave per new block of 16 tokens, 16 of them a
-// round.  Token s of the new cache comes from position list[s] >= s, so that a new block reads from pages at or behind its own: all
-// waves of a round load, then all store, and what later rounds read is still there.
+// Moves the kept tokens to the front, in place.  A block per (head, layer, sequence), a wave per new block of 16 tokens, EM_WAVES of
+// them a round.  Token s of the new cache comes from position list[s] >= s, so that a new block reads from pages at or behind its own:
+// when all waves of a round have what they move, they store, and what later rounds read is still there.  What bounds it is the chain
+// position -> page -> bytes, so a round's bytes are requested before the round in front of it stores (its pages lie behind),
+// page numbers one round and positions two rounds ahead.
 // In units of A / 127 the old values are q * A, exact in fp32 where A has the 16 bits of the model's type; those of the open
 // block are 127 * v.  The new block's magnitude in those units is W: A' = W / 127, q' = rint(value * 127 / W).  All in 32 bits,
 // for 32-bit models and blocks that were evicted before too, whose products are rounded.
-constexpr int EM_WAVES = 16;
+constexpr int EM_WAVES = 8;
 template <typename T, int D>
 __global__ __launch_bounds__(64 * EM_WAVES) void kv8_move_kernel(const Kv8Layer* __restrict__ layers, int n_heads, Kv8Evict e,
                                                                  const int32_t* __restrict__ lists) {
     const int g = blockIdx.x, layer = blockIdx.y, sq = blockIdx.z;
     const int len = e.len[sq], keep = e.keep[sq];
     if (len <= keep) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Kv8Layer kv = layers[layer];
     const int32_t* pt = e.page_tables + (size_t)sq * e.pt_stride;
     const int32_t* list = lists + e.list_off[sq] + ((size_t)layer * n_heads + g) * keep;
@@ -445,93 +485,129 @@ __global__ __launch_bounds__(64 * EM_WAVES) void kv8_move_kernel(const Kv8Layer*
     T* vo = ko + (size_t)n_heads * 16 * D;
     const int full = len / 16;                               // full blocks of the old cache
     const int blocks = (keep + 15) / 16;
-    constexpr int R = D / 64;                                // a lane has elements lane + 64 r of every token
+    constexpr int R = D / 64;                                // a lane has elements R * lane + r of every token
+    // lane t (of 16): position and page of token t of a wave's block; behind the end the last token again
+    auto position = [&](int blk) {
+        const int i = blk * 16 + (lane & 15);
+        return list[i < keep ? i : keep - 1];
+    };
+    struct Raw { uint32_t k[16], v[16][R]; float ak, av, w; };
+    auto fetch = [&](int pos, int page, Raw& x) {
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+            const size_t at = ((size_t)__builtin_amdgcn_readlane(page, t) * n_heads + g) * 16 * D;
+            const int tok = __builtin_amdgcn_readlane(pos, t) & 15;
+            const int8_t *kp = kv.k + at + tok * D, *vp = kv.v + at + tok;
+            x.k[t] = R == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(kp + 2 * lane) : (uint32_t)*reinterpret_cast<const uint8_t*>(kp + lane);
+#pragma unroll
+            for (int r = 0; r < R; ++r) x.v[t][r] = (uint8_t)vp[(R * lane + r) * 16];
+        }
+        const size_t at = (size_t)page * n_heads + g;
+        const float2 a = *reinterpret_cast<const float2*>(kv.amax + at * 2);
+        x.ak = a.x;
+        x.av = a.y;
+        x.w = kv.w[at * 16 + (pos & 15)];
+    };
+    int pos = position(wave), page = pt[pos >> 4], pos_n = position(wave + EM_WAVES);
+    Raw raw;
+    fetch(pos, page, raw);
     for (int b0 = 0; b0 < blocks; b0 += EM_WAVES) {
         const int blk = b0 + wave;
         const int cnt = blk < blocks ? (keep - blk * 16 < 16 ? keep - blk * 16 : 16) : 0;
-        float xk[16][R], xv[16][R], w = 0.f;
-        float mk = 0.f, mv = 0.f;
-#pragma unroll
-        for (int t = 0; t < 16; ++t) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) xk[t][r] = xv[t][r] = 0.f;
-            if (t < cnt) {
-                const int p = list[blk * 16 + t];
-                if (p >= full * 16) {
-#pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        xk[t][r] = ldf(ko + (p & 15) * D + lane + 64 * r);
-                        xv[t][r] = ldf(vo + (p & 15) * D + lane + 64 * r);
-                    }
-                } else {
-                    const size_t page = (size_t)pt[p >> 4] * n_heads + g;
-#pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        xk[t][r] = (float)kv.k[page * 16 * D + (p & 15) * D + lane + 64 * r];
-                        xv[t][r] = (float)kv.v[page * 16 * D + (size_t)(lane + 64 * r) * 16 + (p & 15)];
-                    }
-                }
-            }
-        }
-        // magnitudes of the blocks the tokens come from: lane t has those of token t (127 for the open one, where the value is itself)
-        float ak = 0.f, av = 0.f;
-        if (lane < cnt) {
-            const int p = list[blk * 16 + lane];
-            const size_t page = (size_t)pt[p >> 4] * n_heads + g;
-            ak = p >= full * 16 ? 127.f : kv.amax[page * 2];
-            av = p >= full * 16 ? 127.f : kv.amax[page * 2 + 1];
-            w = kv.w[page * 16 + (p & 15)];
-        }
-        // scaled where a product could pass the largest float
-        const bool open_mine = lane < cnt && ak == 127.f && av == 127.f;
-        float top_k = open_mine ? 0.f : ak, top_v = open_mine ? 0.f : av;
-        const uint64_t opens = __ballot(open_mine);
+        const int page_n = pt[pos_n >> 4], pos_nn = position(blk + 2 * EM_WAVES);
+        const int page_to = blk < blocks ? pt[blk] : 0;
+        // an open block's token: the value is itself, its magnitude stands for 127
+        const bool open_mine = (lane & 15) < cnt && pos >= full * 16;
+        const uint32_t opens = (uint32_t)__ballot(open_mine) & 0xffffu;
+        const float ak = (lane & 15) >= cnt ? 0.f : open_mine ? 127.f : raw.ak, av = (lane & 15) >= cnt ? 0.f : open_mine ? 127.f : raw.av, w = raw.w;
+        float xk[16][R], xv[16][R];
 #pragma unroll
         for (int t = 0; t < 16; ++t)
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+            for (int r = 0; r < R; ++r) {
+                xk[t][r] = (float)(int8_t)(raw.k[t] >> (8 * r));
+                xv[t][r] = (float)(int8_t)raw.v[t][r];
+            }
+        float top_k = open_mine ? 0.f : ak, top_v = open_mine ? 0.f : av;
+        if (opens) {
+#pragma unroll
+            for (int t = 0; t < 16; ++t)
                 if (opens >> t & 1) {
-                    top_k = fmaxf(top_k, fabsf(xk[t][r]));
-                    top_v = fmaxf(top_v, fabsf(xv[t][r]));
+                    const int p = __builtin_amdgcn_readlane(pos, t) & 15;
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        xk[t][r] = ldf(ko + p * D + R * lane + r);
+                        xv[t][r] = ldf(vo + p * D + R * lane + r);
+                        top_k = fmaxf(top_k, fabsf(xk[t][r]));
+                        top_v = fmaxf(top_v, fabsf(xv[t][r]));
+                    }
                 }
+        }
+        // scaled where a product could pass the largest float
         const float fk = kv8_fit(wave_max(top_k)), fv = kv8_fit(wave_max(top_v));
+        float mk = 0.f, mv = 0.f;
 #pragma unroll
         for (int t = 0; t < 16; ++t) {
-            const float sk = __shfl(ak, t, 64) * fk, sv = __shfl(av, t, 64) * fv;
+            const float sk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ak * fk), t));
+            const float sv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(av * fv), t));
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                xk[t][r] *= sk;
-                xv[t][r] *= sv;
+                xk[t][r] = t < cnt ? xk[t][r] * sk : 0.f;
+                xv[t][r] = t < cnt ? xv[t][r] * sv : 0.f;
                 mk = fmaxf(mk, kv8_mag(xk[t][r]));
                 mv = fmaxf(mv, kv8_mag(xv[t][r]));
             }
         }
         mk = wave_max(mk);
         mv = wave_max(mv);
-        __syncthreads();                                     // the round has read what it moves
+        // Complete here: only then are the others let on to store.
+#pragma unroll
+        for (int t = 0; t < 16; ++t)
+#pragma unroll
+            for (int r = 0; r < R; ++r) asm volatile("" : "+v"(xk[t][r]), "+v"(xv[t][r]));
+        float w_to = w;
+        asm volatile("" : "+v"(w_to));
+        pos = pos_n;
+        page = page_n;
+        pos_n = pos_nn;
+        if (b0 + EM_WAVES < blocks) fetch(pos, page, raw);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
         if (cnt > 0) {
-            const size_t page = (size_t)pt[blk] * n_heads + g;
-            if (lane < cnt) kv.w[page * 16 + lane] = w;
+            const size_t to = (size_t)page_to * n_heads + g;
+            if (lane < cnt) kv.w[to * 16 + lane] = w_to;
             if (cnt == 16) {
                 if (lane == 0) {
-                    kv.amax[page * 2] = kv8_amax(mk) / 127.f / fk;
-                    kv.amax[page * 2 + 1] = kv8_amax(mv) / 127.f / fv;
+                    kv.amax[to * 2] = kv8_amax(mk) / 127.f / fk;
+                    kv.amax[to * 2 + 1] = kv8_amax(mv) / 127.f / fv;
                 }
-                const float gk = kv8_fit(mk), gv = kv8_fit(mv);
+                const float gk = kv8_fit(mk), gv = kv8_fit(mv), wk = mk * gk, wv = mv * gv, rk = 1.f / wk, rv = 1.f / wv;
+                int q[R][4];
+#pragma unroll
+                for (int t = 0; t < 16; t += 4) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const float x[4] = {xk[t][r] * gk, xk[t + 1][r] * gk, xk[t + 2][r] * gk, xk[t + 3][r] * gk};
+                        kv8_round_n<bf16_t, 4>(x, wk, rk, q[r]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        int8_t* kp = kv.k + to * 16 * D + (t + j) * D + R * lane;
+                        if constexpr (R == 2) *reinterpret_cast<uint16_t*>(kp) = (uint16_t)((q[0][j] & 255) | q[R - 1][j] << 8);
+                        else *kp = (int8_t)q[0][j];
+                    }
+                }
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     vec16 o;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        int q[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            kv.k[page * 16 * D + (4 * i + j) * D + lane + 64 * r] = (int8_t)kv8_round<bf16_t>(xk[4 * i + j][r] * gk, mk * gk);
-                            q[j] = kv8_round<bf16_t>(xv[4 * i + j][r] * gv, mv * gv);
-                        }
-                        o.w[i] = kv8_pack4(q);
+                    for (int t = 0; t < 16; t += 4) {
+                        const float x[4] = {xv[t][r] * gv, xv[t + 1][r] * gv, xv[t + 2][r] * gv, xv[t + 3][r] * gv};
+                        kv8_round_n<bf16_t, 4>(x, wv, rv, q[r]);
+                        o.w[t / 4] = kv8_pack4(q[r]);
                     }
-                    *reinterpret_cast<vec16*>(kv.v + page * 16 * D + (size_t)(lane + 64 * r) * 16) = o;
+                    *reinterpret_cast<vec16*>(kv.v + to * 16 * D + (size_t)(R * lane + r) * 16) = o;
                 }
             } else {
 #pragma unroll
@@ -539,8 +615,8 @@ __global__ __launch_bounds__(64 * EM_WAVES) void kv8_move_kernel(const Kv8Layer*
                     if (t < cnt)
 #pragma unroll
                         for (int r = 0; r < R; ++r) {
-                            stf(ko + t * D + lane + 64 * r, xk[t][r] / fk / 127.f);
-                            stf(vo + t * D + lane + 64 * r, xv[t][r] / fv / 127.f);
+                            stf(ko + t * D + R * lane + r, xk[t][r] / fk / 127.f);
+                            stf(vo + t * D + R * lane + r, xv[t][r] / fv / 127.f);
                         }
             }
         }
@@ -557,7 +633,7 @@ hipError_t kv8_evict(int dt, const Kv8Layer* layers, int n_heads, int d, const K
     if ((d != 64 && d != 128) || n_heads <= 0 || e.n_layers <= 0 || e.n_layers > 65535 || e.n_seqs > 65535 || !lists || e.recent < 0)
         return hipErrorInvalidValue;
     const dim3 grid(n_heads, e.n_layers, e.n_seqs);
-    kv8_select_kernel<<<grid, EV_T, 0, s>>>(layers, n_heads, e, lists);
+    kv8_select_kernel<<<grid, EV_T, sizeof(uint32_t) * (e.max_len < EV_KEYS ? e.max_len : EV_KEYS), s>>>(layers, n_heads, e, lists);
     SS_TYPED(dt, d, launch_move, (layers, n_heads, e, lists, grid, s));
     return hipGetLastError();
 }
