@@ -22,14 +22,14 @@ template <typename T> __device__ __forceinline__ int kv8_round(float v, float am
 template <typename T, int N>
 __device__ __forceinline__ void kv8_round_n(const float* v, float amax, float rc, int* q) {
     constexpr float FAR = sizeof(T) == 4 ? 0.4989f : 0.4999f;
-    bool far = amax > 0.f && amax < INFINITY;
+    float off = 0.f;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         const float t = v[j] * 127.f * rc, r = rintf(t);
         q[j] = (int)r;
-        far = far && fabsf(t - r) < FAR;
+        off = fmaxf(off, fabsf(t - r));
     }
-    if (!far) {
+    if (!(off < FAR && amax > 1e-30f && amax < INFINITY)) {              // (a smaller one's reciprocal may not be finite)
 #pragma unroll
         for (int j = 0; j < N; ++j) q[j] = kv8_round<T>(v[j], amax);
     }
@@ -467,6 +467,9 @@ __global__ __launch_bounds__(EV_T) void kv8_select_kernel(const Kv8Layer* __rest
 // when all waves of a round have what they move, they store, and what later rounds read is still there.  What bounds it is the chain
 // position -> page -> bytes, so a round's bytes are requested before the round in front of it stores (its pages lie behind),
 // page numbers one round and positions two rounds ahead.
+// A token's V is a byte of every row of its page: the page's rows are brought once, 16 bytes a lane, for all tokens that come from
+// it, and v_perm puts the bytes where they go (one load a token and row instead took twice the time).  Eight pages are requested ahead,
+// which is enough where half of a page or more stays; what lies behind them is waited for.
 // In units of A / 127 the old values are q * A, exact in fp32 where A has the 16 bits of the model's type; those of the open
 // block are 127 * v.  The new block's magnitude in those units is W: A' = W / 127, q' = rint(value * 127 / W).  All in 32 bits,
 // for 32-bit models and blocks that were evicted before too, whose products are rounded.
@@ -491,17 +494,30 @@ __global__ __launch_bounds__(64 * EM_WAVES) void kv8_move_kernel(const Kv8Layer*
         const int i = blk * 16 + (lane & 15);
         return list[i < keep ? i : keep - 1];
     };
-    struct Raw { uint32_t k[16], v[16][R]; float ak, av, w; };
+    constexpr int AHEAD = 8;
+    struct Raw { uint32_t k[16]; vec16 v[AHEAD][R]; float ak, av, w; };
+    // first tokens of the pages that a block comes from
+    auto starts = [&](int pos) { return (uint32_t)__ballot(lane == 0 || pos >> 4 != __shfl_up(pos, 1, 64) >> 4) & 0xffffu; };
+    auto fetch_rows = [&](uint32_t from, int page, vec16 (&rows)[AHEAD][R]) {
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (from) {
+                const size_t at = ((size_t)__builtin_amdgcn_readlane(page, __builtin_ctz(from)) * n_heads + g) * 16 * D;
+                from &= from - 1;
+#pragma unroll
+                for (int r = 0; r < R; ++r) rows[j][r] = *reinterpret_cast<const vec16*>(kv.v + at + (R * lane + r) * 16);
+            }
+        }
+    };
     auto fetch = [&](int pos, int page, Raw& x) {
 #pragma unroll
         for (int t = 0; t < 16; ++t) {
             const size_t at = ((size_t)__builtin_amdgcn_readlane(page, t) * n_heads + g) * 16 * D;
             const int tok = __builtin_amdgcn_readlane(pos, t) & 15;
-            const int8_t *kp = kv.k + at + tok * D, *vp = kv.v + at + tok;
+            const int8_t* kp = kv.k + at + tok * D;
             x.k[t] = R == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(kp + 2 * lane) : (uint32_t)*reinterpret_cast<const uint8_t*>(kp + lane);
-#pragma unroll
-            for (int r = 0; r < R; ++r) x.v[t][r] = (uint8_t)vp[(R * lane + r) * 16];
         }
+        fetch_rows(starts(pos), page, x.v);
         const size_t at = (size_t)page * n_heads + g;
         const float2 a = *reinterpret_cast<const float2*>(kv.amax + at * 2);
         x.ak = a.x;
@@ -520,13 +536,51 @@ __global__ __launch_bounds__(64 * EM_WAVES) void kv8_move_kernel(const Kv8Layer*
         const bool open_mine = (lane & 15) < cnt && pos >= full * 16;
         const uint32_t opens = (uint32_t)__ballot(open_mine) & 0xffffu;
         const float ak = (lane & 15) >= cnt ? 0.f : open_mine ? 127.f : raw.ak, av = (lane & 15) >= cnt ? 0.f : open_mine ? 127.f : raw.av, w = raw.w;
+        // lane 4 j + i: where tokens 4 i .. + 3 come from in a row of the block's j-th page, as selectors of its lower and its upper 8
+        // bytes; 12 is a byte of zeros
+        uint32_t from = starts(pos), sel_lo = 0, sel_hi = 0;
+        const int mine = (__popc(from & ((2u << (lane & 15)) - 1)) - 1) << 4 | (pos & 15);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int x = __shfl(mine, (lane & 3) * 4 + u, 64);
+            const bool here = x >> 4 == lane >> 2;
+            sel_lo |= (here && !(x & 8) ? x & 7 : 12) << (8 * u);
+            sel_hi |= (here && (x & 8) ? x & 7 : 12) << (8 * u);
+        }
+        uint32_t vw[4][R];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < R; ++r) vw[i][r] = 0;
+        auto take = [&](int j0, int n, const vec16 (&rows)[AHEAD][R]) {
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                if (j < n) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t lo = __builtin_amdgcn_readlane(sel_lo, 4 * (j0 + j) + i), hi = __builtin_amdgcn_readlane(sel_hi, 4 * (j0 + j) + i);
+#pragma unroll
+                        for (int r = 0; r < R; ++r)
+                            vw[i][r] |= __builtin_amdgcn_perm(rows[j][r].w[1], rows[j][r].w[0], lo) | __builtin_amdgcn_perm(rows[j][r].w[3], rows[j][r].w[2], hi);
+                    }
+                }
+            }
+        };
+        const int n_from = __popc(from);
+        take(0, n_from, raw.v);
+        if (n_from > AHEAD) {
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) from &= from - 1;
+            fetch_rows(from, page, raw.v);
+            take(AHEAD, n_from - AHEAD, raw.v);
+        }
         float xk[16][R], xv[16][R];
 #pragma unroll
         for (int t = 0; t < 16; ++t)
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 xk[t][r] = (float)(int8_t)(raw.k[t] >> (8 * r));
-                xv[t][r] = (float)(int8_t)raw.v[t][r];
+                xv[t][r] = (float)(int8_t)(vw[t / 4][r] >> (8 * (t & 3)));
             }
         float top_k = open_mine ? 0.f : ak, top_v = open_mine ? 0.f : av;
         if (opens) {
@@ -552,11 +606,24 @@ __global__ __launch_bounds__(64 * EM_WAVES) void kv8_move_kernel(const Kv8Layer*
             const float sv = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(av * fv), t));
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                xk[t][r] = t < cnt ? xk[t][r] * sk : 0.f;
-                xv[t][r] = t < cnt ? xv[t][r] * sv : 0.f;
-                mk = fmaxf(mk, kv8_mag(xk[t][r]));
-                mv = fmaxf(mv, kv8_mag(xv[t][r]));
+                xk[t][r] *= sk;
+                xv[t][r] *= sv;
+                mk = fmaxf(mk, fabsf(xk[t][r]));
+                mv = fmaxf(mv, fabsf(xv[t][r]));
             }
+        }
+        // What fmaxf does not keep: a NaN, of a block whose magnitude is one or of the open block.  In a block that is not full no
+        // magnitude is asked for, and tokens behind the end (0 times whatever is there) are not stored.
+        if (__any(ak != ak)) mk = INFINITY;
+        if (__any(av != av)) mv = INFINITY;
+        if (opens) {
+#pragma unroll
+            for (int t = 0; t < 16; ++t)
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    mk = fmaxf(mk, kv8_mag(xk[t][r]));
+                    mv = fmaxf(mv, kv8_mag(xv[t][r]));
+                }
         }
         mk = wave_max(mk);
         mv = wave_max(mv);
@@ -583,12 +650,21 @@ __global__ __launch_bounds__(64 * EM_WAVES) void kv8_move_kernel(const Kv8Layer*
                     kv.amax[to * 2 + 1] = kv8_amax(mv) / 127.f / fv;
                 }
                 const float gk = kv8_fit(mk), gv = kv8_fit(mv), wk = mk * gk, wv = mv * gv, rk = 1.f / wk, rv = 1.f / wv;
+                if (gk * gv != 1.f) {
+#pragma unroll
+                    for (int t = 0; t < 16; ++t)
+#pragma unroll
+                        for (int r = 0; r < R; ++r) {
+                            xk[t][r] *= gk;
+                            xv[t][r] *= gv;
+                        }
+                }
                 int q[R][4];
 #pragma unroll
                 for (int t = 0; t < 16; t += 4) {
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        const float x[4] = {xk[t][r] * gk, xk[t + 1][r] * gk, xk[t + 2][r] * gk, xk[t + 3][r] * gk};
+                        const float x[4] = {xk[t][r], xk[t + 1][r], xk[t + 2][r], xk[t + 3][r]};
                         kv8_round_n<bf16_t, 4>(x, wk, rk, q[r]);
                     }
 #pragma unroll
@@ -603,7 +679,7 @@ __global__ __launch_bounds__(64 * EM_WAVES) void kv8_move_kernel(const Kv8Layer*
                     vec16 o;
 #pragma unroll
                     for (int t = 0; t < 16; t += 4) {
-                        const float x[4] = {xv[t][r] * gv, xv[t + 1][r] * gv, xv[t + 2][r] * gv, xv[t + 3][r] * gv};
+                        const float x[4] = {xv[t][r], xv[t + 1][r], xv[t + 2][r], xv[t + 3][r]};
                         kv8_round_n<bf16_t, 4>(x, wv, rv, q[r]);
                         o.w[t / 4] = kv8_pack4(q[r]);
                     }
