@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void attn8_generic_kernel(const T* __restrict_
             d += __shfl_xor(d, 2, 64);
             s[t] = j * 16 + t <= p ? d : -INFINITY;
             mx = fmaxf(mx, s[t]);
-            if (scores && valid && sub == 0 && j * 16 + t <= p) scores[((size_t)b.tok_off[sq] + j * 16 + t) * n_q + a] = s[t];
+            if (scores && valid && sub == 0 && j * 16 + t <= p) scores[(((size_t)b.pg_off[sq] + j) * n_q + a) * 16 + t] = s[t];
         }
         // position 0 is seen by every query: mx is finite from the first page on, unless the scores are not
         const float ref = mx == -INFINITY ? 0.f : mx;
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float r = -INFINITY, l = 0.f;                                        // reference of the exponents, sum in its units
-    float* sp = WEIGHTS ? scores + (size_t)b.tok_off[sq] * n_q + a : nullptr;
+    float* sp = WEIGHTS ? scores + ((size_t)b.pg_off[sq] * n_q + a) * 16 : nullptr;      // [page][n_q][16]
 
     auto rescale = [&](float top) {
         const float alpha = exp2_fast(r - top);
@@ -261,8 +261,11 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
                 for (int v = 0; v < 4; ++v) {
                     s[i][v] = whole || 4 * i + v <= seen ? s[i][v] * ks : -INFINITY;
                     top = fmaxf(top, s[i][v]);
-                    if (WEIGHTS && mine && 4 * i + v <= seen) sp[(size_t)(pg * 16 + 4 * i + v) * n_q] = s[i][v];
                 }
+            if (WEIGHTS && mine && seen >= 0) {                          // those behind the last token are not read
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4_t*>(sp + (size_t)pg * n_q * 16 + 4 * i) = s[i];
+            }
             top = over_groups(top + lv) - TOP_EXP;
             if (__any(top > r)) rescale(fmaxf(top, r));
             const float off = lv - r;
@@ -339,8 +342,8 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
         for (int v = 0; v < 4; ++v) {
             s[v] = 4 * g4 + v < cnt ? s[v] * scale_log2e : -INFINITY;
             top = fmaxf(top, s[v]);
-            if (WEIGHTS && mine && 4 * g4 + v < cnt) sp[(size_t)(full * 16 + 4 * g4 + v) * n_q] = s[v];
         }
+        if (WEIGHTS && mine) *reinterpret_cast<f32x4_t*>(sp + (size_t)full * n_q * 16 + 4 * g4) = s;
         rescale(fmaxf(r, over_groups(top + lv) - TOP_EXP));
         float rs = 0.f;
 #pragma unroll
@@ -376,16 +379,21 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
     }
 }
 
-// Merge of the items' partial results: D / 4 threads per (query head, sequence), HB heads a block; four items are requested together.
-template <int D, int HB>
-__global__ __launch_bounds__(D / 4 * HB) void attn8_merge_kernel(const float* __restrict__ scratch, bf16_t* __restrict__ out, int n_q, Kv8Batch b,
-                                                                 float* __restrict__ lse) {
-    const int sq = blockIdx.y, e = threadIdx.x % (D / 4) * 4, a = blockIdx.x * HB + threadIdx.x / (D / 4);
+// Merge of the items' partial results: D / 4 threads (a row) per query head, SPLIT rows of a block share the items of one, four of which
+// are requested together.  With 8 rows a head, long caches (70 items) take 6 us less; where a row has few items, one row a head is shorter.
+template <int D, int SPLIT>
+__global__ __launch_bounds__(256) void attn8_merge_kernel(const float* __restrict__ scratch, bf16_t* __restrict__ out, int n_q, Kv8Batch b,
+                                                          float* __restrict__ lse) {
+    constexpr int ROWS = 1024 / D;
+    static_assert(SPLIT == 1 || SPLIT == ROWS, "");
+    __shared__ float part[SPLIT > 1 ? SPLIT : 1][D + 4];
+    const int sq = blockIdx.y, e = threadIdx.x % (D / 4) * 4, row = threadIdx.x / (D / 4);
+    const int a = SPLIT > 1 ? blockIdx.x : blockIdx.x * ROWS + row, step = SPLIT > 1 ? 4 * SPLIT : 4;
     if (a >= n_q) return;
-    const int i0 = b.wk.seq_item0[sq], i1 = b.wk.seq_item0[sq + 1];
+    const int i0 = b.wk.seq_item0[sq] + (SPLIT > 1 ? row * 4 : 0), i1 = b.wk.seq_item0[sq + 1];
     float M = -INFINITY, den = 0.f;
     f32x4_t num = {0.f, 0.f, 0.f, 0.f};
-    for (int i = i0; i < i1; i += 4) {
+    for (int i = i0; i < i1; i += step) {
         float m[4], l[4];
         f32x4_t v[4];
 #pragma unroll
@@ -417,6 +425,25 @@ __global__ __launch_bounds__(D / 4 * HB) void attn8_merge_kernel(const float* __
             den += w * l[u];
         }
     }
+    if constexpr (SPLIT > 1) {
+        *reinterpret_cast<f32x4_t*>(&part[row][e]) = num;
+        if (e == 0) { part[row][D] = M; part[row][D + 1] = den; }
+        __syncthreads();
+        if (row > 0) return;
+        float mx = M;
+#pragma unroll
+        for (int u = 1; u < SPLIT; ++u) mx = fmaxf(mx, part[u][D]);
+        const float ref = mx == -INFINITY ? 0.f : mx, w0 = exp2_fast(M - ref);
+        M = mx;
+        num *= w0;
+        den *= w0;
+#pragma unroll
+        for (int u = 1; u < SPLIT; ++u) {
+            const float w = exp2_fast(part[u][D] - ref);
+            num += w * *reinterpret_cast<const f32x4_t*>(&part[u][e]);
+            den += w * part[u][D + 1];
+        }
+    }
     vec16 w;
     w.w[0] = pack_bf16x2(num[0] / den, num[1] / den);
     w.w[1] = pack_bf16x2(num[2] / den, num[3] / den);
@@ -432,7 +459,9 @@ static void launch_decode(const void* q, int64_t q_stride, void* out, int n_q, i
     const unsigned grid = (unsigned)((long long)b.wk.n_items * n_kv * n_ct);
     const auto kernel = scores ? attn8_decode_kernel<D, true> : attn8_decode_kernel<D, false>;
     kernel<<<grid, 64, 0, s>>>((const bf16_t*)q, q_stride, n_q, n_kv, n_ct, b, kv, scratch, scores, sl2);
-    attn8_merge_kernel<D, 1024 / D><<<dim3((n_q * D + 1023) / 1024, b.n_seqs), 256, 0, s>>>(scratch, (bf16_t*)out, n_q, b, lse);
+    constexpr int ROWS = 1024 / D;
+    if (b.wk.max_items_per_seq > ROWS) attn8_merge_kernel<D, ROWS><<<dim3(n_q, b.n_seqs), 256, 0, s>>>(scratch, (bf16_t*)out, n_q, b, lse);
+    else attn8_merge_kernel<D, 1><<<dim3((n_q + ROWS - 1) / ROWS, b.n_seqs), 256, 0, s>>>(scratch, (bf16_t*)out, n_q, b, lse);
 }
 
 // ---------------------------------------------------------------- prompts
@@ -755,23 +784,33 @@ hipError_t attn8_prefill(int dt, const void* q, int64_t q_stride, void* out, int
 }
 
 // ---------------------------------------------------------------- accumulated weights
-// A thread per (token, kv head): the weights of the head's G queries, in their order, onto what is there.
+// A thread per (four tokens, kv head): the weights of the head's G queries, in their order, onto what is there.
 __global__ __launch_bounds__(256) void attn8_weights_kernel(const float* __restrict__ scores, const float* __restrict__ lse, int n_q, int n_kv,
                                                             Kv8Batch b, float* __restrict__ w) {
-    const int sq = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x, t = i / n_kv, g = i % n_kv;
-    if (t > b.before[sq]) return;
+    const int sq = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x, t4 = i % 4 * 4, g = i / 4 % n_kv, pg = i / 4 / n_kv, before = b.before[sq];
+    if (pg * 16 + t4 > before) return;
     const int G = n_q / n_kv;
-    const float* sp = scores + ((size_t)b.tok_off[sq] + t) * n_q + g * G;
+    const float* sp = scores + (((size_t)b.pg_off[sq] + pg) * n_q + g * G) * 16 + t4;
     const float* lp = lse + (size_t)sq * n_q + g * G;
-    float sum = 0.f;
-    for (int j = 0; j < G; ++j) sum += exp2_fast(sp[j] - lp[j]);
-    w[((size_t)b.page_tables[(size_t)sq * b.pt_stride + t / 16] * n_kv + g) * 16 + t % 16] += sum;
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int j = 0; j < G; ++j) {
+        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(sp + j * 16);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sum[v] += exp2_fast(x[v] - lp[j]);
+    }
+    f32x4_t* wp = reinterpret_cast<f32x4_t*>(w + ((size_t)b.page_tables[(size_t)sq * b.pt_stride + pg] * n_kv + g) * 16 + t4);
+    f32x4_t x = *wp;
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+        if (pg * 16 + t4 + v <= before) x[v] += sum[v];
+    *wp = x;
 }
 
-// partial results [n_items][n_q][d + 4], then (weights) the logarithms [n_seqs][n_q] and the scores [tokens seen][n_q]
+// partial results [n_items][n_q][d + 4], then (weights) the scores [pages seen][n_q][16] and the logarithms [n_seqs][n_q]
 static size_t partial_floats(const Kv8Batch& b, int n_q, int d) { return (size_t)b.wk.n_items * n_q * (d + 4); }
 size_t attn8_decode_scratch_floats(const Kv8Batch& b, int n_q, int d, bool weights) {
-    return partial_floats(b, n_q, d) + (weights ? (size_t)b.n_seqs * n_q + (size_t)b.seen * n_q : 0);
+    return partial_floats(b, n_q, d) + (weights ? (size_t)b.n_seqs * n_q + (size_t)b.seen_pages * n_q * 16 : 0);
 }
 
 hipError_t attn8_decode(int dt, const void* q, int64_t q_stride, void* out, int n_q, int n_kv, int d, const Kv8Batch& b,
@@ -779,8 +818,8 @@ hipError_t attn8_decode(int dt, const void* q, int64_t q_stride, void* out, int 
     if (b.n_seqs <= 0) return hipSuccess;
     if (!attn8_fits(n_q, n_kv, d, b, q, q_stride, dt) || b.max_q_len != 1 || !scratch) return hipErrorInvalidValue;
     if ((long long)b.max_seen * n_kv > 0x7fffff00ll) return hipErrorInvalidValue;
-    float* lse = kv.w ? scratch + partial_floats(b, n_q, d) : nullptr;
-    float* scores = kv.w ? lse + (size_t)b.n_seqs * n_q : nullptr;
+    float* scores = kv.w ? scratch + partial_floats(b, n_q, d) : nullptr;
+    float* lse = kv.w ? scores + (size_t)b.seen_pages * n_q * 16 : nullptr;
     hipError_t e = hipSuccess;
     if (dt == F32 || force_generic) {
         e = attn8_generic(dt, q, q_stride, out, n_q, n_kv, d, b, kv, scores, lse, s);
@@ -791,7 +830,7 @@ hipError_t attn8_decode(int dt, const void* q, int64_t q_stride, void* out, int 
         e = hipGetLastError();
     }
     if (e != hipSuccess || !kv.w) return e;
-    attn8_weights_kernel<<<dim3((unsigned)(((long long)b.max_seen * n_kv + 255) / 256), b.n_seqs), 256, 0, s>>>(scores, lse, n_q, n_kv, b, kv.w);
+    attn8_weights_kernel<<<dim3((unsigned)(((long long)(b.max_seen + 15) / 16 * 4 * n_kv + 255) / 256), b.n_seqs), 256, 0, s>>>(scores, lse, n_q, n_kv, b, kv.w);
     return hipGetLastError();
 }
 

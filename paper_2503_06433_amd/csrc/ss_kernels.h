@@ -129,9 +129,9 @@ struct Kv8Batch {
     const int32_t* end;          // [n_seqs] cached tokens of the layer once the batch's are in: blocks below end / 16 are full
     const int32_t* slot;         // [n_seqs]
     const int32_t* pos;          // [n_seqs]
-    const int32_t* tok_off;      // [n_seqs] tokens that the sequences in front see (weights only)
+    const int32_t* pg_off;       // [n_seqs] pages that the sequences in front see (weights only)
     int n_seqs, T, max_q_len, max_seen;
-    int64_t seen;                // tokens that all sequences see
+    int64_t seen_pages;          // pages that all sequences see
     const int32_t* unit_seq;     // page units of the new tokens, as in BatchMeta
     const int32_t* unit_tok0;
     const int32_t* unit_pos0;

@@ -1215,7 +1215,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
         if (need > pages) more += need - pages;
         fresh += !st;
         T += ql;
-        seen += cached + ql;
+        seen += (cached + ql + ps - 1) / ps;
         max_q = std::max(max_q, ql);
         max_seen = std::max(max_seen, cached + ql);
     }
@@ -1224,7 +1224,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
             for (int j = 0; j < i; ++j)
                 if (b->seq_ids[j] == b->seq_ids[i]) return fail(c, SS_EINVAL, "sequence %lld is listed twice", (long long)b->seq_ids[i]);
     if (T > (1 << 30) || (int64_t)max_q * (s->nq_l / s->nkv_l) > (1 << 30)) return fail(c, SS_EINVAL, "batch too large");
-    if (decode && s->kv8_weights && seen > INT32_MAX) return fail(c, SS_EINVAL, "batch too large: it sees %lld tokens", (long long)seen);
+    if (decode && s->kv8_weights && seen > INT32_MAX) return fail(c, SS_EINVAL, "batch too large: it sees %lld pages", (long long)seen);
     if (more > s->free_pages.size())
         return fail(c, SS_ENOMEM, "page pool exhausted: the batch needs %zu more pages, %zu free", more, s->free_pages.size());
     if (fresh > s->free_slots.size())
@@ -1250,7 +1250,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
     // ---- build
     int pt_stride = 1;
     std::vector<const SeqState*> sts(n);
-    std::vector<int32_t> cu(n + 1), tok_off(n);
+    std::vector<int32_t> cu(n + 1), pg_off(n);
     int32_t t = 0, o = 0;
     for (int i = 0; i < n; ++i) {
         sts[i] = &s->seqs[b->seq_ids[i]];
@@ -1258,7 +1258,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
         pt_stride = std::max<int>(pt_stride, (int)sts[i]->pages.size());
         cu[i] = t;
         t += b->q_lens[i];
-        if (decode && s->kv8_weights) { tok_off[i] = o; o += before[i] + 1; }
+        if (decode && s->kv8_weights) { pg_off[i] = o; o += before[i] / ps + 1; }
     }
     cu[n] = t;
     std::vector<int32_t> pt((size_t)n * pt_stride, 0);
@@ -1299,7 +1299,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
     if (!decode && c->dt != SS_F32) prefill8_items(c, s, n, cu, before, end, &pf, &pf_stride, &pf_blocks);
     Image im;
     const size_t o_cu = im.add(cu), o_before = im.add(before), o_end = im.add(end), o_slot = im.add(slot), o_pos = im.add(pos),
-                 o_tok = im.add(tok_off), o_pt = im.add(pt), o_us = im.add(unit_seq), o_ut = im.add(unit_tok0), o_up = im.add(unit_pos0),
+                 o_tok = im.add(pg_off), o_pt = im.add(pt), o_us = im.add(unit_seq), o_ut = im.add(unit_tok0), o_up = im.add(unit_pos0),
                  o_uc = im.add(unit_cnt), o_is = im.add(item_seq), o_ip = im.add(item_page0), o_in = im.add(item_np), o_si = im.add(seq_item0),
                  o_io = im.add(item_order), o_pf = im.add(pf);
     Meta8Slot* ms = nullptr;
@@ -1310,8 +1310,8 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
     ssk::Kv8Batch& k = ms->b;
     k = {};
     k.page_tables = at(o_pt); k.pt_stride = pt_stride;
-    k.cu_q = at(o_cu); k.before = at(o_before); k.end = at(o_end); k.slot = at(o_slot); k.pos = at(o_pos); k.tok_off = at(o_tok);
-    k.n_seqs = n; k.T = (int)T; k.max_q_len = max_q; k.max_seen = max_seen; k.seen = seen;
+    k.cu_q = at(o_cu); k.before = at(o_before); k.end = at(o_end); k.slot = at(o_slot); k.pos = at(o_pos); k.pg_off = at(o_tok);
+    k.n_seqs = n; k.T = (int)T; k.max_q_len = max_q; k.max_seen = max_seen; k.seen_pages = seen;
     k.unit_seq = at(o_us); k.unit_tok0 = at(o_ut); k.unit_pos0 = at(o_up); k.unit_cnt = at(o_uc); k.n_units = (int)unit_seq.size();
     k.pf_items = pf.empty() ? nullptr : at(o_pf); k.pf_stride = pf_stride; k.pf_blocks = pf_blocks;
     k.wk.item_seq = at(o_is); k.wk.item_page0 = at(o_ip); k.wk.item_npages = at(o_in); k.wk.seq_item0 = at(o_si); k.wk.item_order = at(o_io);
