@@ -486,12 +486,9 @@ __device__ __forceinline__ float max_of_halves(float x) {
 __device__ __forceinline__ float neighbour(float x) {
     return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0xb1, 0xf, 0xf, true));
 }
-// one instruction; fmaxf would first make its operands from the matrix cores canonical, one by one
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
+// One instruction.  fmaxf would first make its operands from the matrix cores canonical, one by one, because it does not keep a NaN; a
+// row with one is NaN whatever this returns.
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 
 // The reference of a row's exponents follows the largest only when that has grown by more than LAG: the largest weight is 2^TOP_ROW
 // to 2^(TOP_ROW + LAG) (half: 2^15, see TOP_EXP).
@@ -524,245 +521,292 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
     const uint32_t v_read = KBYTES + g2 * (D * 32) + lq * 32 + (lq >> 3 & 1) * 16;
     auto lds = [&](uint32_t at) { return reinterpret_cast<vec16*>(smem + at); };
 
-    for (int pj = 0;; ++pj) {
-        const int32_t* rec = b.pf_items + ((size_t)blockIdx.x * b.pf_stride + pj) * 8;
-        const int sq = __builtin_amdgcn_readfirstlane(rec[0]);
-        if (sq < 0) break;                                               // end of the list: the whole block leaves
-        const int g = __builtin_amdgcn_readfirstlane(rec[1]), row0 = __builtin_amdgcn_readfirstlane(rec[2]);
-        const int q_begin = __builtin_amdgcn_readfirstlane(rec[3]), rows = __builtin_amdgcn_readfirstlane(rec[4]) * G;
-        const int before = __builtin_amdgcn_readfirstlane(rec[5]), end = __builtin_amdgcn_readfirstlane(rec[6]);
-        const int full = end / 16;
+    // Two walks over the block's items: this one brings tiles, three ahead of the other, which multiplies them, and goes on to the next
+    // item's while the other is at the last ones of its own.  Records come one item ahead, an element a lane.
+    const int32_t* items = b.pf_items + (size_t)blockIdx.x * b.pf_stride * 8 + (lane & 7);
+    auto field = [](int rec, int i) { return __builtin_amdgcn_readlane(rec, i); };
+    int rec = items[0], rec_b = rec;
+    if (field(rec, 0) < 0) return;
+    // a lane holds what belongs to page lane / 32 of a tile or, odd lanes, the second behind it
+    const int my_page = g2 + 2 * (lane & 1);
+    struct Ids { int page, g; };
+    int b_tile = 0, b_pages = 0, b_g = 0, b_next = 0;
+    const int32_t* b_pt = nullptr;
+    auto b_item = [&] {
+        b_pt = b.page_tables + (size_t)field(rec_b, 0) * b.pt_stride;
+        b_g = field(rec_b, 1);
+        b_pages = field(rec_b, 7);
+        b_tile = 0;
+        rec_b = items[++b_next * 8];                                     // behind the last record is one that says so
+    };
+    b_item();
+    auto load_ids = [&] {
+        const int j = b_tile * 4 + my_page;
+        const Ids r{b_pt[j < b_pages ? j : b_pages - 1], b_g};
+        if (++b_tile * 4 >= b_pages) {
+            if (field(rec_b, 0) >= 0) b_item();
+            else --b_tile;                                               // the last tile again and again, for nobody
+        }
+        return r;
+    };
+    struct Raw { vec16 k, v; float2 amax; };
+    auto load_raw = [&](const Ids& ids, Raw& w) {
+        const size_t page = ((size_t)__builtin_amdgcn_readlane(ids.page, (pg_w & 1) * 32 + (pg_w >> 1)) * n_kv + ids.g) * 16 * D;
+        uint32_t at = unit * 16;                                         // 32 bits next to a scalar base, not two 64-bit addresses a lane
+        asm volatile("" : "+v"(at));
+        if (does_k) w.k = *reinterpret_cast<const vec16*>(kv.k + page + at);
+        if (does_v) w.v = *reinterpret_cast<const vec16*>(kv.v + page + at);
+        w.amax = *reinterpret_cast<const float2*>(kv.amax + ((size_t)ids.page * n_kv + ids.g) * 2);
+    };
+    struct Steps { float ks, lv, inv; };                                 // of the lane's page
+    uint32_t stage = 0;                                                  // of the tile that is multiplied; the next one is in the other
+    // LDS image of the next tile; returns the steps of its pages
+    auto store = [&](uint32_t st, const Raw& w) {
+        Steps s;
+        s.ks = w.amax.x * (ONE_127 * scale_log2e);
+        s.ks = s.ks < 1e-37f ? 1e-37f : s.ks;                            // a block of zeros: any step, but no infinity times zero
+        v_step(w.amax.y, s.lv, s.inv);
+        if (does_k) {
+            *lds(st + k_write) = widen8(w.k.w[0], w.k.w[1]).q;
+            *lds((st + k_write) ^ 16) = widen8(w.k.w[2], w.k.w[3]).q;
+        }
+        if (does_v) {
+            *lds(st + v_write) = widen8(w.v.w[0], w.v.w[1]).q;
+            *lds((st + v_write) ^ 16) = widen8(w.v.w[2], w.v.w[3]).q;
+        }
+        return s;
+    };
+    auto publish = [] {                                                  // what this wave wrote is there before the others are let on
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    // the item that is multiplied
+    int g, p, end, full, n_tiles, open_tile, wave_first, wave_last, sq, bad;
+    bool valid, active;
+    int64_t op;
+    half8_t qf[KS];
+    int at = 0;
+    auto begin = [&] {
+        sq = field(rec, 0);
+        if (sq < 0) return false;
+        g = field(rec, 1);
+        const int row0 = field(rec, 2), q_begin = field(rec, 3), rows = field(rec, 4) * G, before = field(rec, 5), n_pages = field(rec, 7);
+        end = field(rec, 6);
+        rec = items[++at * 8];
+        full = end / 16;
+        n_tiles = (n_pages + 3) / 4;
+        open_tile = full < n_pages ? full >> 2 : -1;
         const int wrow = row0 + wave * 32, row = wrow + lq;
-        const bool valid = row < rows, active = wrow < rows;
-        const int qi = (valid ? row : row0) / G, head = g * G + (valid ? row : row0) % G;
-        const int p = before + qi;
-        const int wave_first = before + wrow / G, wave_last = before + (wrow + 31 < rows ? wrow + 31 : rows - 1) / G;
-        const int blk_last = before + (row0 + 255 < rows ? row0 + 255 : rows - 1) / G;
-        const int n_pages = blk_last / 16 + 1, n_tiles = (n_pages + 3) / 4;
-        const int32_t* pt = b.page_tables + (size_t)sq * b.pt_stride;
+        valid = row < rows;
+        active = wrow < rows;
+        const int qi = (valid ? row : row0) / G, head = g * G + (valid ? row : row0) - qi * G;
+        p = before + qi;
+        wave_first = before + wrow / G;
+        wave_last = before + (wrow + 31 < rows ? wrow + 31 : rows - 1) / G;
+        bad = 0;
+        op = ((int64_t)(q_begin + qi) * n_q + head) * D;
+        const bf16_t* qp = q + (int64_t)(q_begin + qi) * q_stride + (size_t)head * D + g2 * 8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const half8_t*>(qp + ks * 16);
+        return true;
+    };
+    f32x16_t o[DT];
+    float r, l;
+
+    // The open block's page of the tile that is multiplied next, over what `store` brought there: the model's type as it is, V times a
+    // power of two that brings it below 128 and without values that are not finite; tokens that have such are marked, their
+    // weight is to be NaN.
+    auto store_open = [&](uint32_t st, Steps& s) {
         const bf16_t* ko = (const bf16_t*)kv.open + ((size_t)b.slot[sq] * 2 * n_kv + g) * 16 * D;
         const bf16_t* vo = ko + (size_t)n_kv * 16 * D;
-
-        half8_t qf[KS];
-        {
-            const bf16_t* qp = q + (int64_t)(q_begin + qi) * q_stride + (size_t)head * D + g2 * 8;
+        const int cnt = end - full * 16;
+        float big = 0.f;
+        int mark = 0;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const half8_t*>(qp + ks * 16);
+        for (int i = 0; i < D / 32; ++i) {                           // all of V by every wave: all need its step
+            const int at = (i * 64 + lane) * 8, tok = at / D;
+            if (tok < cnt) {
+                float x[8];
+                unpack16<bf16_t>(*reinterpret_cast<const vec16*>(vo + at), x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool fin = fabsf(x[e]) < INFINITY;
+                    big = fmaxf(big, fin ? fabsf(x[e]) : 0.f);
+                    mark |= fin ? 0 : 1 << tok;
+                }
+            }
         }
-        f32x16_t o[DT];
+        big = wave_max(big);
+#pragma unroll
+        for (int i = 32; i > 0; i >>= 1) mark |= __shfl_xor(mark, i, 64);
+        bad = mark;
+        int e = big > 0.f ? (int)(__float_as_uint(big) >> 23) - 127 - 6 : (int)LV_ZERO;
+        e = e < (int)LV_MIN ? (int)LV_MIN : e;
+        if (my_page == (full & 3)) s = Steps{scale_log2e, (float)e, exp2_fast((float)-e)};
+        if ((full & 3) != pg_w) return;
+        if (does_k) {
+            const vec16* kr = reinterpret_cast<const vec16*>(ko + k_tok * D + k_piece * 16);
+            *lds(st + k_write) = kr[0];
+            *lds((st + k_write) ^ 16) = kr[1];
+        }
+        if (does_v) {
+            const float down = exp2_fast((float)-e);
+            float x[16];
+#pragma unroll
+            for (int t = 0; t < 16; ++t) {
+                x[t] = t < cnt ? bf2f(vo[t * D + unit]) : 0.f;
+                x[t] = fabsf(x[t]) < INFINITY ? x[t] * down : 0.f;
+            }
+            Frag8 lo, hi;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                lo.w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+                hi.w[i] = pack_bf16x2(x[8 + 2 * i], x[9 + 2 * i]);
+            }
+            *lds(st + v_write) = lo.q;
+            *lds((st + v_write) ^ 16) = hi.q;
+        }
+    };
+
+    // 32 tokens of scores, of the lane's page 16, become weights.  `hidden`: some of them are not to be seen by every row.
+    auto softmax = [&](auto hidden_c, f32x16_t& s, float ks, float lv, float inv, int t0, Frag8& pA, Frag8& pB) {
+        constexpr bool hidden = decltype(hidden_c)::value;
+        if constexpr (hidden) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[v] = t0 + v <= p ? s[v] : -INFINITY;
+        }
+        float m = max3(s[0], s[1], s[2]);
+#pragma unroll
+        for (int v = 3; v < 15; v += 2) m = max3(m, s[v], s[v + 1]);
+        const float top = max_of_halves(fmaf(fmaxf(m, s[15]), ks, lv)) - TOP_ROW;
+        const bool moved = top - r > LAG;                            // also in the first step (r = -infinity)
+        const float alpha = moved ? exp2_fast(r - top) : 1.f;
+        r = moved ? top : r;
+        const float off = lv - r;
+        float sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            s[v] = exp2_fast(fmaf(s[v], ks, off));
+            if constexpr (hidden) {                                  // the steps of a block that is not seen may not be numbers
+                s[v] = t0 + v <= p ? s[v] : 0.f;
+                if (bad && t0 + v >= full * 16 && t0 + v <= p && (bad >> (t0 + v - full * 16) & 1)) s[v] = __uint_as_float(0x7fc00000u);
+            }
+            sum += s[v];
+        }
+        sum *= inv;
+        l = l * alpha + (hidden && t0 > p ? 0.f : sum);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            pA.w[i] = pack_bf16x2(s[2 * i], s[2 * i + 1]);
+            pB.w[i] = pack_bf16x2(s[8 + 2 * i], s[9 + 2 * i]);
+        }
+        // complete here, not wherever their first use is moved to
+        asm volatile("" : "+v"(pA.w[0]), "+v"(pA.w[1]), "+v"(pA.w[2]), "+v"(pA.w[3]), "+v"(pB.w[0]), "+v"(pB.w[1]), "+v"(pB.w[2]), "+v"(pB.w[3]));
+        return alpha;
+    };
+    auto rescale = [&](float alpha) {
+        if (__builtin_expect(__any(alpha != 1.f), 0)) {              // said to be rare, so that the other path needs no copies of o
+#pragma unroll
+            for (int u = 0; u < DT; ++u)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[u][v] *= alpha;
+        }
+    };
+    // One tile; the scores of its second half are asked for in front of the softmax of the first, so that products and vector
+    // operations can stand side by side.
+    auto tile = [&](auto hidden_c, int it, const Steps& st) {
+        constexpr bool hidden = decltype(hidden_c)::value;
+        const uint32_t kp = stage + k_read, vp = stage + v_read;
+        auto read_k = [&](int h, int ks) { return *reinterpret_cast<const half8_t*>(lds((kp ^ (ks * 32)) + h * 32 * ROW)); };
+        auto read_v = [&](int h, int i) { return *reinterpret_cast<const half8_t*>(lds((vp ^ (i & 1) * 16) + h * D * 64 + (i >> 1) * 1024)); };
+        const float ks_n = neighbour(st.ks), lv_n = neighbour(st.lv), inv_n = neighbour(st.inv);
+        const bool odd = lane & 1;
+        const int t0 = it * 64 + g2 * 16;
+        f32x16_t s0, s1;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s0[v] = s1[v] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s0 = SS_MFMA_32x32x16(read_k(0, ks), qf[ks], s0, 0, 0, 0);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s1 = SS_MFMA_32x32x16(read_k(1, ks), qf[ks], s1, 0, 0, 0);
+        Frag8 pA, pB;
+        float alpha = softmax(hidden_c, s0, odd ? ks_n : st.ks, odd ? lv_n : st.lv, odd ? inv_n : st.inv, t0, pA, pB);
+        rescale(alpha);
+#pragma unroll
+        for (int i = 0; i < KS; ++i) o[i >> 1] = SS_MFMA_32x32x16(read_v(0, i), i & 1 ? pB.v : pA.v, o[i >> 1], 0, 0, 0);
+        Frag8 pC, pD;
+        alpha = softmax(hidden_c, s1, odd ? st.ks : ks_n, odd ? st.lv : lv_n, odd ? st.inv : inv_n, t0 + 32, pC, pD);
+        rescale(alpha);
+#pragma unroll
+        for (int i = 0; i < KS; ++i) o[i >> 1] = SS_MFMA_32x32x16(read_v(1, i), i & 1 ? pD.v : pC.v, o[i >> 1], 0, 0, 0);
+    };
+
+    Ids ids = load_ids();
+    Raw raw;
+    load_raw(ids, raw);
+    ids = load_ids();
+    begin();
+    Steps cur = store(0, raw);
+    load_raw(ids, raw);
+    ids = load_ids();
+    publish();
+    for (;;) {
 #pragma unroll
         for (int u = 0; u < DT; ++u)
 #pragma unroll
             for (int v = 0; v < 16; ++v) o[u][v] = 0.f;
-        float r = -INFINITY, l = 0.f;
-
-        // a lane holds what belongs to page lane / 32 of a tile or, odd lanes, the second behind it
-        const int my_page = g2 + 2 * (lane & 1);
-        struct Raw { vec16 k, v; float2 amax; };
-        auto load_ids = [&](int tile) {
-            const int j = tile * 4 + my_page;
-            return pt[j < n_pages ? j : n_pages - 1];
-        };
-        auto load_raw = [&](int ids, Raw& w) {
-            const size_t page = ((size_t)__builtin_amdgcn_readlane(ids, (pg_w & 1) * 32 + (pg_w >> 1)) * n_kv + g) * 16 * D;
-            uint32_t at = unit * 16;                                     // 32 bits next to a scalar base, not two 64-bit addresses a lane
-            asm volatile("" : "+v"(at));
-            if (does_k) w.k = *reinterpret_cast<const vec16*>(kv.k + page + at);
-            if (does_v) w.v = *reinterpret_cast<const vec16*>(kv.v + page + at);
-            w.amax = *reinterpret_cast<const float2*>(kv.amax + ((size_t)ids * n_kv + g) * 2);
-        };
-        struct Steps { float ks, lv, inv; };                             // of the lane's page
-        // LDS image of a tile; returns the steps of its pages
-        auto store = [&](int tile, const Raw& w) {
-            const uint32_t st = (tile & 1) * STAGE;
-            Steps s;
-            s.ks = w.amax.x * (ONE_127 * scale_log2e);
-            s.ks = s.ks < 1e-37f ? 1e-37f : s.ks;                         // a block of zeros: any step, but no infinity times zero
-            v_step(w.amax.y, s.lv, s.inv);
-            if (does_k) {
-                *lds(st + k_write) = widen8(w.k.w[0], w.k.w[1]).q;
-                *lds((st + k_write) ^ 16) = widen8(w.k.w[2], w.k.w[3]).q;
-            }
-            if (does_v) {
-                *lds(st + v_write) = widen8(w.v.w[0], w.v.w[1]).q;
-                *lds((st + v_write) ^ 16) = widen8(w.v.w[2], w.v.w[3]).q;
-            }
-            return s;
-        };
-        // The open block's page of a tile, over what `store` brought there: the model's type as it is, V times a power of two that brings it below 128 and without values
-        // that are not finite; tokens that have such are marked, their weight is to be NaN.
-        int bad = 0;
-        auto store_open = [&](int tile, Steps& s) {
-            const int cnt = end - full * 16;
-            float big = 0.f;
-            int mark = 0;
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) {                           // all of V by every wave: all need its step
-                const int at = (i * 64 + lane) * 8, tok = at / D;
-                if (tok < cnt) {
-                    float x[8];
-                    unpack16<bf16_t>(*reinterpret_cast<const vec16*>(vo + at), x);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const bool fin = fabsf(x[e]) < INFINITY;
-                        big = fmaxf(big, fin ? fabsf(x[e]) : 0.f);
-                        mark |= fin ? 0 : 1 << tok;
-                    }
-                }
-            }
-            big = wave_max(big);
-#pragma unroll
-            for (int i = 32; i > 0; i >>= 1) mark |= __shfl_xor(mark, i, 64);
-            bad = mark;
-            int e = big > 0.f ? (int)(__float_as_uint(big) >> 23) - 127 - 6 : (int)LV_ZERO;
-            e = e < (int)LV_MIN ? (int)LV_MIN : e;
-            if (my_page == (full & 3)) s = Steps{scale_log2e, (float)e, exp2_fast((float)-e)};
-            if ((full & 3) != pg_w) return;
-            const uint32_t st = (tile & 1) * STAGE;
-            if (does_k) {
-                const vec16* kr = reinterpret_cast<const vec16*>(ko + k_tok * D + k_piece * 16);
-                *lds(st + k_write) = kr[0];
-                *lds((st + k_write) ^ 16) = kr[1];
-            }
-            if (does_v) {
-                const float down = exp2_fast((float)-e);
-                float x[16];
-#pragma unroll
-                for (int t = 0; t < 16; ++t) {
-                    x[t] = t < cnt ? bf2f(vo[t * D + unit]) : 0.f;
-                    x[t] = fabsf(x[t]) < INFINITY ? x[t] * down : 0.f;
-                }
-                Frag8 lo, hi;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    lo.w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
-                    hi.w[i] = pack_bf16x2(x[8 + 2 * i], x[9 + 2 * i]);
-                }
-                *lds(st + v_write) = lo.q;
-                *lds((st + v_write) ^ 16) = hi.q;
-            }
-        };
-
-        // 32 tokens of scores, of the lane's page 16, become weights.  `hidden`: some of them are not to be seen by every row.
-        auto softmax = [&](auto hidden_c, f32x16_t& s, float ks, float lv, float inv, int t0, Frag8& pA, Frag8& pB) {
-            constexpr bool hidden = decltype(hidden_c)::value;
-            if constexpr (hidden) {
-#pragma unroll
-                for (int v = 0; v < 16; ++v) s[v] = t0 + v <= p ? s[v] : -INFINITY;
-            }
-            float m = max3(s[0], s[1], s[2]);
-#pragma unroll
-            for (int v = 3; v < 15; v += 2) m = max3(m, s[v], s[v + 1]);
-            const float top = max_of_halves(fmaf(fmaxf(m, s[15]), ks, lv)) - TOP_ROW;
-            const bool moved = top - r > LAG;                            // also in the first step (r = -infinity)
-            const float alpha = moved ? exp2_fast(r - top) : 1.f;
-            r = moved ? top : r;
-            const float off = lv - r;
-            float sum = 0.f;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                s[v] = exp2_fast(fmaf(s[v], ks, off));
-                if constexpr (hidden) {                                  // the steps of a block that is not seen may not be numbers
-                    s[v] = t0 + v <= p ? s[v] : 0.f;
-                    if (bad && t0 + v >= full * 16 && t0 + v <= p && (bad >> (t0 + v - full * 16) & 1)) s[v] = __uint_as_float(0x7fc00000u);
-                }
-                sum += s[v];
-            }
-            sum *= inv;
-            l = l * alpha + (hidden && t0 > p ? 0.f : sum);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                pA.w[i] = pack_bf16x2(s[2 * i], s[2 * i + 1]);
-                pB.w[i] = pack_bf16x2(s[8 + 2 * i], s[9 + 2 * i]);
-            }
-            // complete here, not wherever their first use is moved to
-            asm volatile("" : "+v"(pA.w[0]), "+v"(pA.w[1]), "+v"(pA.w[2]), "+v"(pA.w[3]), "+v"(pB.w[0]), "+v"(pB.w[1]), "+v"(pB.w[2]), "+v"(pB.w[3]));
-            return alpha;
-        };
-        auto rescale = [&](float alpha) {
-            if (__builtin_expect(__any(alpha != 1.f), 0)) {              // said to be rare, so that the other path needs no copies of o
-#pragma unroll
-                for (int u = 0; u < DT; ++u)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) o[u][v] *= alpha;
-            }
-        };
-        auto publish = [] {                                              // what this wave wrote is there before the others are let on
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        };
-
-        // One tile; the scores of its second half are asked for in front of the softmax of the first, so that products and vector
-        // operations can stand side by side.
-        auto tile = [&](auto hidden_c, int it, const Steps& st) {
-            constexpr bool hidden = decltype(hidden_c)::value;
-            const uint32_t kp = (it & 1) * STAGE + k_read, vp = (it & 1) * STAGE + v_read;
-            auto read_k = [&](int h, int ks) { return *reinterpret_cast<const half8_t*>(lds((kp ^ (ks * 32)) + h * 32 * ROW)); };
-            auto read_v = [&](int h, int i) { return *reinterpret_cast<const half8_t*>(lds((vp ^ (i & 1) * 16) + h * D * 64 + (i >> 1) * 1024)); };
-            const float ks_n = neighbour(st.ks), lv_n = neighbour(st.lv), inv_n = neighbour(st.inv);
-            const bool odd = lane & 1;
-            const int t0 = it * 64 + g2 * 16;
-            f32x16_t s0, s1;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) s0[v] = s1[v] = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s0 = SS_MFMA_32x32x16(read_k(0, ks), qf[ks], s0, 0, 0, 0);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s1 = SS_MFMA_32x32x16(read_k(1, ks), qf[ks], s1, 0, 0, 0);
-            Frag8 pA, pB;
-            float alpha = softmax(hidden_c, s0, odd ? ks_n : st.ks, odd ? lv_n : st.lv, odd ? inv_n : st.inv, t0, pA, pB);
-            rescale(alpha);
-#pragma unroll
-            for (int i = 0; i < KS; ++i) o[i >> 1] = SS_MFMA_32x32x16(read_v(0, i), i & 1 ? pB.v : pA.v, o[i >> 1], 0, 0, 0);
-            Frag8 pC, pD;
-            alpha = softmax(hidden_c, s1, odd ? st.ks : ks_n, odd ? st.lv : lv_n, odd ? st.inv : inv_n, t0 + 32, pC, pD);
-            rescale(alpha);
-#pragma unroll
-            for (int i = 0; i < KS; ++i) o[i >> 1] = SS_MFMA_32x32x16(read_v(1, i), i & 1 ? pD.v : pC.v, o[i >> 1], 0, 0, 0);
-        };
-
-        int ids = load_ids(0);
-        Raw raw;
-        load_raw(ids, raw);
-        ids = load_ids(1);
-        Steps cur = store(0, raw), nxt = cur;
-        if (full < 4 && full < n_pages) store_open(0, cur);
-        load_raw(ids, raw);
-        ids = load_ids(2);
-        publish();
-        // Behind the last tile the last pages are brought once more, to a stage that nobody reads.
-        auto bring = [&](int it) {
-            nxt = store(it + 1, raw);
+        r = -INFINITY;
+        l = 0.f;
+        Steps nxt;
+        auto bring = [&] {
+            nxt = store(stage ^ STAGE, raw);
             load_raw(ids, raw);
-            ids = load_ids(it + 3);
-            if (full >> 2 == it + 1 && full < n_pages) store_open(it + 1, nxt);
+            ids = load_ids();
+        };
+        auto next = [&] {
+            cur = nxt;
+            stage ^= STAGE;
+            publish();
         };
         // first the tiles that every row of the wave sees all of
         int it = 0;
         for (; it < n_tiles && active && it * 64 + 63 <= wave_first; ++it) {
-            bring(it);
+            bring();
             tile(std::false_type{}, it, cur);
-            cur = nxt;
-            publish();
+            next();
         }
         for (; it < n_tiles; ++it) {
-            bring(it);
+            bring();
+            if (it == open_tile) {
+                store_open(stage, cur);
+                publish();
+            }
             if (active && it * 64 <= wave_last) tile(std::true_type{}, it, cur);
-            cur = nxt;
-            publish();
+            next();
         }
         l += __shfl_xor(l, 32, 64);
-        if (valid) {
-            const float inv = 1.f / l;
-            bf16_t* op = out + ((size_t)(q_begin + qi) * n_q + head) * D;
+        const float inv = 1.f / l;
+        bf16_t* to = out + op;
+        const bool stores = valid, more = begin();                       // the next item's queries are requested
+        if (stores) {
 #pragma unroll
             for (int u = 0; u < DT; ++u)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    *reinterpret_cast<uint2*>(op + u * 32 + 8 * j + 4 * g2) =
-                        make_uint2(pack_bf16x2(o[u][4 * j] * inv, o[u][4 * j + 1] * inv), pack_bf16x2(o[u][4 * j + 2] * inv, o[u][4 * j + 3] * inv));
+                for (int j = 0; j < 4; j += 2) {                         // lane halves hold 4 elements each of 8: one takes the even 8, one the odd
+                    vec16 w;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[u][4 * j + 2 * i] * inv, o[u][4 * j + 2 * i + 1] * inv),
+                                                                        pack_bf16x2(o[u][4 * j + 4 + 2 * i] * inv, o[u][4 * j + 5 + 2 * i] * inv), false, false);
+                        w.w[i] = x[0];
+                        w.w[2 + i] = x[1];
+                    }
+                    *reinterpret_cast<vec16*>(to + u * 32 + 8 * (j + g2)) = w;
+                }
         }
+        if (!more) break;
     }
 }
 

@@ -1053,9 +1053,11 @@ int run_attn_phase(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, 
 }
 
 // ------------------------------------------------------------------ caches in 8 bits
-// Pages per work item of a decode step over a cache in 8 bits, a multiple of the four that the kernel takes at a time.
+// Pages per work item of a decode step over a cache in 8 bits, a multiple of the four that the kernel takes at a time: 2048 waves or
+// more where there are that many pages (six long sequences with half as many: 137 us instead of 135, with twice as many 130, but 150
+// instead of 147 for 1024 sequences of one head), and no more than 256 of them (256 sequences of 32 heads: 535 us, 548 at 128, 565 at 64).
 static int decode8_item_pages(int64_t total_pages, int n_kv_local) {
-    const int64_t n = std::max<int64_t>(16, std::min<int64_t>(64, total_pages * n_kv_local / 2048));
+    const int64_t n = std::max<int64_t>(8, std::min<int64_t>(256, total_pages * n_kv_local / 2048));
     return (int)(n & ~3);
 }
 
@@ -1167,7 +1169,8 @@ void prefill8_items(ss_ctx* c, Shard* s, int n, const std::vector<int32_t>& cu, 
             const Item& it = lists[blk][j];
             int32_t* r = &(*out)[(blk * stride + j) * 8];
             r[0] = it.sq; r[1] = it.g; r[2] = it.row0; r[3] = cu[it.sq]; r[4] = cu[it.sq + 1] - cu[it.sq];
-            r[5] = before[it.sq]; r[6] = end[it.sq]; r[7] = 0;
+            r[5] = before[it.sq]; r[6] = end[it.sq];
+            r[7] = (r[5] + (std::min(it.row0 + 255, r[4] * G - 1)) / G) / 16 + 1;
         }
 }
 
