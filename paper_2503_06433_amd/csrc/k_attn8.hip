@@ -499,7 +499,7 @@ template <int D> constexpr int prefill_stage = 2 * 64 * D * 2;
 
 template <int D>
 __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __restrict__ q, int64_t q_stride, bf16_t* __restrict__ out, int n_q,
-                                                            int n_kv, Kv8Batch b, Kv8Layer kv, float scale_log2e) {
+                                                            int n_kv, Kv8Batch b, Kv8Layer kv, float scale_log2e, float* __restrict__ scratch) {
     constexpr int KS = D / 16, DT = D / 32, ROW = 2 * D, KBYTES = 64 * ROW, STAGE = prefill_stage<D>;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int G = n_q / n_kv;
@@ -523,7 +523,7 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
 
     // Two walks over the block's items: this one brings tiles, three ahead of the other, which multiplies them, and goes on to the next
     // item's while the other is at the last ones of its own.  Records come one item ahead, an element a lane.
-    const int32_t* items = b.pf_items + (size_t)blockIdx.x * b.pf_stride * 8 + (lane & 7);
+    const int32_t* items = b.pf_items + (size_t)blockIdx.x * b.pf_stride * 16 + (lane & 15);
     auto field = [](int rec, int i) { return __builtin_amdgcn_readlane(rec, i); };
     int rec = items[0], rec_b = rec;
     if (field(rec, 0) < 0) return;
@@ -536,8 +536,8 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
         b_pt = b.page_tables + (size_t)field(rec_b, 0) * b.pt_stride;
         b_g = field(rec_b, 1);
         b_pages = field(rec_b, 7);
-        b_tile = 0;
-        rec_b = items[++b_next * 8];                                     // behind the last record is one that says so
+        b_tile = field(rec_b, 8);
+        rec_b = items[++b_next * 16];                                    // behind the last record is one that says so
     };
     b_item();
     auto load_ids = [&] {
@@ -583,7 +583,7 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
     };
 
     // the item that is multiplied
-    int g, p, end, full, n_tiles, open_tile, wave_first, wave_last, sq, bad;
+    int g, p, end, full, tile0, n_tiles, open_tile, wave_first, wave_last, sq, bad, part;
     bool valid, active;
     int64_t op;
     half8_t qf[KS];
@@ -594,7 +594,9 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
         g = field(rec, 1);
         const int row0 = field(rec, 2), q_begin = field(rec, 3), rows = field(rec, 4) * G, before = field(rec, 5), n_pages = field(rec, 7);
         end = field(rec, 6);
-        rec = items[++at * 8];
+        tile0 = field(rec, 8);
+        part = field(rec, 9);
+        rec = items[++at * 16];
         full = end / 16;
         n_tiles = (n_pages + 3) / 4;
         open_tile = full < n_pages ? full >> 2 : -1;
@@ -606,7 +608,7 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
         wave_first = before + wrow / G;
         wave_last = before + (wrow + 31 < rows ? wrow + 31 : rows - 1) / G;
         bad = 0;
-        op = ((int64_t)(q_begin + qi) * n_q + head) * D;
+        op = part < 0 ? ((int64_t)(q_begin + qi) * n_q + head) * D : ((int64_t)part * 256 + wave * 32 + lq) * (D + 4);
         const bf16_t* qp = q + (int64_t)(q_begin + qi) * q_stride + (size_t)head * D + g2 * 8;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const half8_t*>(qp + ks * 16);
@@ -771,7 +773,7 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
             publish();
         };
         // first the tiles that every row of the wave sees all of
-        int it = 0;
+        int it = tile0;
         for (; it < n_tiles && active && it * 64 + 63 <= wave_first; ++it) {
             bring();
             tile(std::false_type{}, it, cur);
@@ -788,9 +790,17 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
         }
         l += __shfl_xor(l, 32, 64);
         const float inv = 1.f / l;
-        bf16_t* to = out + op;
-        const bool stores = valid, more = begin();                       // the next item's queries are requested
-        if (stores) {
+        const int64_t to = op;
+        const bool whole = part < 0, stores = valid, more = begin();     // the next item's queries are requested
+        if (stores && !whole) {
+            float* po = scratch + to;
+#pragma unroll
+            for (int u = 0; u < DT; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<f32x4_t*>(po + u * 32 + 8 * j + 4 * g2) = f32x4_t{o[u][4 * j], o[u][4 * j + 1], o[u][4 * j + 2], o[u][4 * j + 3]};
+            if (g2 == 0) { po[D] = r; po[D + 1] = l; }
+        } else if (stores) {
 #pragma unroll
             for (int u = 0; u < DT; ++u)
 #pragma unroll
@@ -803,28 +813,55 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
                         w.w[i] = x[0];
                         w.w[2 + i] = x[1];
                     }
-                    *reinterpret_cast<vec16*>(to + u * 32 + 8 * (j + g2)) = w;
+                    *reinterpret_cast<vec16*>(out + to + u * 32 + 8 * (j + g2)) = w;
                 }
         }
         if (!more) break;
     }
 }
 
+// Items that were cut: their parts' sums (o, reference, l of 256 rows each) together.  D / 4 threads a row.
 template <int D>
-static hipError_t launch_prefill(const void* q, int64_t q_stride, void* out, int n_q, int n_kv, const Kv8Batch& b, const Kv8Layer& kv, hipStream_t s) {
+__global__ __launch_bounds__(256) void attn8_join_kernel(const float* __restrict__ scratch, bf16_t* __restrict__ out, int n_q, int n_kv, Kv8Batch b) {
+    constexpr int ROWS = 1024 / D;
+    const int32_t* rec = b.pf_cuts + blockIdx.x * 8;                     // sequence, kv head, first row, first query, rows, first part, parts
+    const int G = n_q / n_kv, e = threadIdx.x % (D / 4) * 4, i = blockIdx.y * ROWS + threadIdx.x / (D / 4), row = rec[2] + i;
+    if (row >= rec[4] * G) return;
+    const float* sp = scratch + ((size_t)rec[5] * 256 + i) * (D + 4);
+    float M = -INFINITY, den = 0.f;
+    f32x4_t num = {0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < rec[6]; ++u, sp += 256 * (D + 4)) {
+        const float m = sp[D], l = sp[D + 1];
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(sp + e);
+        const float mx = fmaxf(M, m), ref = mx == -INFINITY ? 0.f : mx, alpha = exp2_fast(M - ref), w = exp2_fast(m - ref);
+        M = mx;
+        num = num * alpha + w * v;
+        den = den * alpha + w * l;
+    }
+    *reinterpret_cast<uint2*>(out + ((int64_t)(rec[3] + row / G) * n_q + rec[1] * G + row % G) * D + e) =
+        make_uint2(pack_bf16x2(num[0] / den, num[1] / den), pack_bf16x2(num[2] / den, num[3] / den));
+}
+
+template <int D>
+static hipError_t launch_prefill(const void* q, int64_t q_stride, void* out, int n_q, int n_kv, const Kv8Batch& b, const Kv8Layer& kv, float* scratch,
+                                 hipStream_t s) {
     constexpr int LDS = 2 * prefill_stage<D>;
     const float sl2 = 1.4426950408889634f / sqrtf((float)D);
-    attn8_prefill_kernel<D><<<(unsigned)b.pf_blocks, 512, LDS, s>>>((const bf16_t*)q, q_stride, (bf16_t*)out, n_q, n_kv, b, kv, sl2);
+    attn8_prefill_kernel<D><<<(unsigned)b.pf_blocks, 512, LDS, s>>>((const bf16_t*)q, q_stride, (bf16_t*)out, n_q, n_kv, b, kv, sl2, scratch);
+    if (b.n_cuts > 0) attn8_join_kernel<D><<<dim3((unsigned)b.n_cuts, D / 4), 256, 0, s>>>(scratch, (bf16_t*)out, n_q, n_kv, b);
     return hipGetLastError();
 }
 
+size_t attn8_prefill_scratch_floats(const Kv8Batch& b, int d) { return (size_t)b.n_parts * 256 * (d + 4); }
+
 hipError_t attn8_prefill(int dt, const void* q, int64_t q_stride, void* out, int n_q, int n_kv, int d, const Kv8Batch& b,
-                         const Kv8Layer& kv, bool force_generic, hipStream_t s) {
+                         const Kv8Layer& kv, float* scratch, bool force_generic, hipStream_t s) {
     if (b.T <= 0 || b.n_seqs <= 0) return hipSuccess;
     if (!attn8_fits(n_q, n_kv, d, b, q, q_stride, dt)) return hipErrorInvalidValue;
     if (dt == F32 || force_generic) return attn8_generic(dt, q, q_stride, out, n_q, n_kv, d, b, kv, nullptr, nullptr, s);
-    if (!b.pf_items || b.pf_blocks <= 0) return hipErrorInvalidValue;
-    return d == 64 ? launch_prefill<64>(q, q_stride, out, n_q, n_kv, b, kv, s) : launch_prefill<128>(q, q_stride, out, n_q, n_kv, b, kv, s);
+    if (!b.pf_items || b.pf_blocks <= 0 || (b.n_parts > 0 && !scratch)) return hipErrorInvalidValue;
+    return d == 64 ? launch_prefill<64>(q, q_stride, out, n_q, n_kv, b, kv, scratch, s)
+                   : launch_prefill<128>(q, q_stride, out, n_q, n_kv, b, kv, scratch, s);
 }
 
 // ---------------------------------------------------------------- accumulated weights

@@ -137,11 +137,14 @@ struct Kv8Batch {
     const int32_t* unit_pos0;
     const int32_t* unit_cnt;
     int n_units;
-    // work lists of prompts: block b walks the records pf_items[(b * pf_stride + j) * 8 .. +7] = (sequence, kv head, first row of a block of
-    // 256, first batch token of the sequence, its new tokens, before, end, 0) up to a sequence of -1; row r is query head r % G of
-    // the kv head's G, token r / G
+    // work lists of prompts: block b walks the records pf_items[(b * pf_stride + j) * 16 .. +15] = (sequence, kv head, first row of a block of
+    // 256, first batch token of the sequence, its new tokens, before, end, pages up to the last that is visited, first tile of four
+    // pages, part or -1) up to a sequence of -1; row r is query head r % G of the kv head's G, token r / G.  An item that is cut leaves its
+    // parts' sums in scratch; pf_cuts[i * 8 .. +7] = (sequence, kv head, first row, first batch token, new tokens, first part, parts, 0)
     const int32_t* pf_items;
     int pf_stride, pf_blocks;
+    const int32_t* pf_cuts;
+    int n_cuts, n_parts;
     DecodeWork wk;               // pages include the open block's
 };
 
@@ -289,7 +292,8 @@ hipError_t kv8_evict(int dt, const Kv8Layer* layers, int n_heads, int d, const K
 
 // Causal attention of the batch's queries over the cache (which has their tokens).  q: rows `q_stride` elements apart, out [T, n_q d].
 hipError_t attn8_prefill(int dt, const void* q, int64_t q_stride, void* out, int n_q, int n_kv, int d, const Kv8Batch& b,
-                         const Kv8Layer& kv, bool force_generic, hipStream_t s);
+                         const Kv8Layer& kv, float* scratch, bool force_generic, hipStream_t s);
+size_t attn8_prefill_scratch_floats(const Kv8Batch& b, int d);
 
 // One query per sequence.  With kv.w the weights of all query heads are added to it.  scratch: attn8_decode_scratch_floats.
 size_t attn8_decode_scratch_floats(const Kv8Batch& b, int n_q, int d, bool weights);

@@ -1120,13 +1120,21 @@ struct Image {
 
 // Work lists of the prompts' attention over a cache in 8 bits.  An item is 256 rows of one (sequence, kv head), a row a query of one
 // of the head's query heads; it costs the tiles of 64 tokens it visits and a fixed part.  Blocks (one per compute
-// unit) are dealt to the XCDs by their index modulo 8.  The items are taken pair by pair, the longest sequence first, the last rows
-// first, and cut into eight shares of equal cost: those that read the same pages mostly share an L2, and few long
-// sequences still fill the chip.  Within a share each goes to the block with the least work so far.
+// unit) are dealt to the XCDs by their index modulo 8.
+// Many items: they are taken pair by pair, the longest sequence first, the last rows first, and cut into eight shares of equal cost, so
+// that those that read the same pages mostly share an L2.  Within a share each goes to the block with the least work so far.
+// Fewer than eight a block: what bounds the time is the block with the most tiles.  Items of more than 1.15 times the mean (and of more than
+// 1024 tokens) are cut into parts along the keys, and each goes to the block with the least work of all.  Chunks of 500 tokens behind
+// 1000 - 6000, 32 heads, where the longest of 256 items is 1.8 times the mean: 203 us uncut, 158 + 5 cut so; half as long or
+// shorter, the parts' sums cost more than is won (+ 25 us).  The same with each kv head's items on one XCD took as long.
+struct Prefill8 {
+    std::vector<int32_t> items, cuts;
+    int stride = 0, blocks = 0, n_parts = 0;
+};
 void prefill8_items(ss_ctx* c, Shard* s, int n, const std::vector<int32_t>& cu, const std::vector<int32_t>& before, const std::vector<int32_t>& end,
-                    std::vector<int32_t>* out, int* stride_out, int* blocks_out) {
-    struct Item { int32_t sq, g, row0, cost; };
-    const int G = s->nq_l / s->nkv_l, per_x = std::max(1, c->n_cus / 8);
+                    Prefill8* out) {
+    struct Item { int32_t sq, g, row0, pages, tile0, part; int cost() const { return (pages + 3) / 4 - tile0 + 3; } };
+    const int G = s->nq_l / s->nkv_l, per_x = std::max(1, c->n_cus / 8), n_blocks = 8 * per_x;
     std::vector<int32_t> order(n);
     for (int i = 0; i < n; ++i) order[i] = i;
     std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return before[x] + cu[x + 1] - cu[x] > before[y] + cu[y + 1] - cu[y]; });
@@ -1137,40 +1145,73 @@ void prefill8_items(ss_ctx* c, Shard* s, int n, const std::vector<int32_t>& cu, 
         for (int g = 0; g < s->nkv_l; ++g)
             for (int64_t r0 = (rows - 1) / 256 * 256; r0 >= 0; r0 -= 256) {
                 const int last = before[i] + (int)(std::min(r0 + 255, rows - 1) / G);
-                items.push_back({i, g, (int32_t)r0, last / 64 + 3});
-                total += items.back().cost;
+                items.push_back({i, g, (int32_t)r0, last / 16 + 1, 0, -1});
+                total += items.back().cost();
             }
     }
-    std::vector<std::vector<Item>> lists((size_t)8 * per_x);
+    std::vector<std::vector<Item>> lists((size_t)n_blocks);
+    // whoever has the least gets the next; returns what it then has
     typedef std::pair<int64_t, int> Load;
-    std::priority_queue<Load, std::vector<Load>, std::greater<Load>> load;
-    int x = -1;
-    int64_t done = 0;
-    for (const Item& it : items) {
-        const int to = (int)std::min<int64_t>(7, (done + it.cost / 2) * 8 / total);
-        if (to != x) {
-            x = to;
-            load = {};
-            for (int k = 0; k < per_x; ++k) load.push({0, k});
+    struct Least : std::priority_queue<Load, std::vector<Load>, std::greater<Load>> {
+        void reset(int n) {
+            c.clear();
+            for (int k = 0; k < n; ++k) push({0, k});
         }
-        const Load top = load.top();
-        load.pop();
-        lists[(size_t)top.second * 8 + x].push_back(it);
-        load.push({top.first + it.cost, top.second});
-        done += it.cost;
+        Load give(int64_t cost) {
+            Load t = top();
+            pop();
+            t.first += cost;
+            push(t);
+            return t;
+        }
+    } least;
+    if (items.size() < (size_t)8 * n_blocks) {
+        const int most = (int)std::max<int64_t>(16, (total * 23 + 20 * n_blocks - 1) / (20 * n_blocks));
+        std::vector<Item> pieces;
+        for (const Item& it : items) {
+            const int tiles = (it.pages + 3) / 4;
+            if (tiles <= most) {
+                pieces.push_back(it);
+                continue;
+            }
+            const int k = (tiles + most - 1) / most;
+            for (int32_t x : {it.sq, it.g, it.row0, cu[it.sq], cu[it.sq + 1] - cu[it.sq], out->n_parts, k, 0}) out->cuts.push_back(x);
+            for (int j = 0; j < k; ++j) {
+                Item p = it;
+                p.tile0 = (int)((int64_t)tiles * j / k);
+                p.pages = std::min<int>(it.pages, (int)((int64_t)tiles * (j + 1) / k) * 4);
+                p.part = out->n_parts++;
+                pieces.push_back(p);
+            }
+        }
+        std::stable_sort(pieces.begin(), pieces.end(), [](const Item& x, const Item& y) { return x.cost() > y.cost(); });
+        lists.resize(std::min(lists.size(), pieces.size()));
+        least.reset((int)lists.size());
+        for (const Item& it : pieces) lists[(size_t)least.give(it.cost()).second].push_back(it);
+    } else {
+        int x = -1;
+        int64_t done = 0;
+        for (const Item& it : items) {
+            const int to = (int)std::min<int64_t>(7, (done + it.cost() / 2) * 8 / total);
+            if (to != x) {
+                x = to;
+                least.reset(per_x);
+            }
+            lists[(size_t)least.give(it.cost()).second * 8 + x].push_back(it);
+            done += it.cost();
+        }
     }
     size_t longest = 0;
     for (const auto& l : lists) longest = std::max(longest, l.size());
-    const int stride = *stride_out = (int)longest + 1;
-    *blocks_out = 8 * per_x;
-    out->assign((size_t)lists.size() * stride * 8, -1);
+    const int stride = out->stride = (int)longest + 1;
+    out->blocks = (int)lists.size();
+    out->items.assign(lists.size() * stride * 16, -1);
     for (size_t blk = 0; blk < lists.size(); ++blk)
         for (size_t j = 0; j < lists[blk].size(); ++j) {
             const Item& it = lists[blk][j];
-            int32_t* r = &(*out)[(blk * stride + j) * 8];
+            int32_t* r = &out->items[(blk * stride + j) * 16];
             r[0] = it.sq; r[1] = it.g; r[2] = it.row0; r[3] = cu[it.sq]; r[4] = cu[it.sq + 1] - cu[it.sq];
-            r[5] = before[it.sq]; r[6] = end[it.sq];
-            r[7] = (r[5] + (std::min(it.row0 + 255, r[4] * G - 1)) / G) / 16 + 1;
+            r[5] = before[it.sq]; r[6] = end[it.sq]; r[7] = it.pages; r[8] = it.tile0; r[9] = it.part;
         }
 }
 
@@ -1297,14 +1338,13 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
         for (size_t i = 0; i < item_order.size(); ++i) item_order[i] = (int32_t)i;
         std::stable_sort(item_order.begin(), item_order.end(), [&](int32_t x, int32_t y) { return (item_np[x] & 0xffff) > (item_np[y] & 0xffff); });
     }
-    std::vector<int32_t> pf;
-    int pf_stride = 0, pf_blocks = 0;
-    if (!decode && c->dt != SS_F32) prefill8_items(c, s, n, cu, before, end, &pf, &pf_stride, &pf_blocks);
+    Prefill8 pf;
+    if (!decode && c->dt != SS_F32) prefill8_items(c, s, n, cu, before, end, &pf);
     Image im;
     const size_t o_cu = im.add(cu), o_before = im.add(before), o_end = im.add(end), o_slot = im.add(slot), o_pos = im.add(pos),
                  o_tok = im.add(pg_off), o_pt = im.add(pt), o_us = im.add(unit_seq), o_ut = im.add(unit_tok0), o_up = im.add(unit_pos0),
                  o_uc = im.add(unit_cnt), o_is = im.add(item_seq), o_ip = im.add(item_page0), o_in = im.add(item_np), o_si = im.add(seq_item0),
-                 o_io = im.add(item_order), o_pf = im.add(pf);
+                 o_io = im.add(item_order), o_pf = im.add(pf.items), o_pc = im.add(pf.cuts);
     Meta8Slot* ms = nullptr;
     int rc = meta8_slot(c, im.total, &ms);
     if (rc) return rc;
@@ -1316,7 +1356,8 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
     k.cu_q = at(o_cu); k.before = at(o_before); k.end = at(o_end); k.slot = at(o_slot); k.pos = at(o_pos); k.pg_off = at(o_tok);
     k.n_seqs = n; k.T = (int)T; k.max_q_len = max_q; k.max_seen = max_seen; k.seen_pages = seen;
     k.unit_seq = at(o_us); k.unit_tok0 = at(o_ut); k.unit_pos0 = at(o_up); k.unit_cnt = at(o_uc); k.n_units = (int)unit_seq.size();
-    k.pf_items = pf.empty() ? nullptr : at(o_pf); k.pf_stride = pf_stride; k.pf_blocks = pf_blocks;
+    k.pf_items = pf.items.empty() ? nullptr : at(o_pf); k.pf_stride = pf.stride; k.pf_blocks = pf.blocks;
+    k.pf_cuts = at(o_pc); k.n_cuts = (int)pf.cuts.size() / 8; k.n_parts = pf.n_parts;
     k.wk.item_seq = at(o_is); k.wk.item_page0 = at(o_ip); k.wk.item_npages = at(o_in); k.wk.seq_item0 = at(o_si); k.wk.item_order = at(o_io);
     k.wk.n_items = (int)item_seq.size(); k.wk.max_items_per_seq = max_items;
     ms->shard = s; ms->version = s->version; ms->decode = decode; ms->write = write;
@@ -1331,8 +1372,10 @@ int run_attn8(ss_ctx* c, Shard* s, int ll, Meta8Slot* ms, bool decode, const voi
     const int d = c->m.head_dim;
     const ssk::Kv8Layer& kv = s->kv8_layers[ll];
     if (!decode) {
+        const int rc = ms->b.n_parts ? ensure_buf(c, c->ws_scratch, sizeof(float) * ssk::attn8_prefill_scratch_floats(ms->b, d)) : SS_OK;
+        if (rc) return rc;
         ProfScope ps(c, 1, st);
-        K_TRY(c, SSK_CALL(c, attn8_prefill, q, q_stride, out, s->nq_l, s->nkv_l, d, ms->b, kv, c->force_generic, st));
+        K_TRY(c, SSK_CALL(c, attn8_prefill, q, q_stride, out, s->nq_l, s->nkv_l, d, ms->b, kv, (float*)c->ws_scratch.p, c->force_generic, st));
         return SS_OK;
     }
     const int rc = ensure_buf(c, c->ws_scratch, sizeof(float) * ssk::attn8_decode_scratch_floats(ms->b, s->nq_l, d, s->kv8_weights));
