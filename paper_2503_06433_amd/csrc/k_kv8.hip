@@ -691,8 +691,8 @@ __global__ __launch_bounds__(64 * EM_WAVES) void kv8_move_kernel(const Kv8Layer*
                     if (t < cnt)
 #pragma unroll
                         for (int r = 0; r < R; ++r) {
-                            stf(ko + t * D + R * lane + r, xk[t][r] / fk / 127.f);
-                            stf(vo + t * D + R * lane + r, xv[t][r] / fv / 127.f);
+                            stf(ko + t * D + R * lane + r, xk[t][r] / 127.f / fk);
+                            stf(vo + t * D + R * lane + r, xv[t][r] / 127.f / fv);
                         }
             }
         }
