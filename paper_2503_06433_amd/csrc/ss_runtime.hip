@@ -1053,12 +1053,13 @@ int run_attn_phase(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, 
 }
 
 // ------------------------------------------------------------------ caches in 8 bits
-// Pages per work item of a decode step over a cache in 8 bits, a multiple of the four that the kernel takes at a time: 2048 waves or
-// more where there are that many pages (six long sequences with half as many: 137 us instead of 135, with twice as many 130, but 150
-// instead of 147 for 1024 sequences of one head), and no more than 256 of them (256 sequences of 32 heads: 535 us, 548 at 128, 565 at 64).
+// Pages per work item of a decode step over a cache in 8 bits, a multiple of the four that the kernel takes at a time: as many waves as
+// the chip holds at once (2048) where there are pages enough.  Six long sequences of 8 heads: 129 us, with half as many waves 142, with
+// twice as many 132; 1024 sequences of one head: 149, 157, 153.  No more than 256 pages: 256 sequences of 32 heads take 535 us, at 128
+// 548, at 64 565.
 static int decode8_item_pages(int64_t total_pages, int n_kv_local) {
-    const int64_t n = std::max<int64_t>(8, std::min<int64_t>(256, total_pages * n_kv_local / 2048));
-    return (int)(n & ~3);
+    const int64_t n = (total_pages * n_kv_local + 2047) / 2048;
+    return (int)(std::max<int64_t>(8, std::min<int64_t>(256, n + 3)) & ~3);
 }
 
 int refuse_capture(ss_ctx* c, hipStream_t st) {
