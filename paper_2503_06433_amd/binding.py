@@ -155,6 +155,9 @@ EXPORTED = ("ss_create ss_destroy ss_last_error ss_load_layer ss_host_weights_pu
 W_NAMES = ("g1", "wq", "wk", "wv", "wo", "g2", "wg", "wu", "wd")     # index = SS_W_* of the header
 
 
+_TYPES = {"torch.float32": SS_F32, "torch.bfloat16": SS_BF16, "torch.float16": SS_F16}
+
+
 def _ptr(x):
     """Raw address of a torch tensor, a numpy array, or an int."""
     if x is None:
@@ -170,10 +173,23 @@ def _rows(x, width):
     """Address and row stride, in elements, of [tokens, heads, d] or [tokens, heads * d] with the heads back to back."""
     if x is None:
         return None, 0
-    row = x[0] if x.shape[0] else x.new_empty(x.shape[1:])
-    if row.numel() != width or not row.is_contiguous():
-        raise ValueError("rows of %d elements expected, heads back to back, not %s with strides %s" % (width, tuple(x.shape), x.stride()))
-    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else width
+    shape, strides, n = x.shape, x.stride(), 1
+    together = True
+    for size, stride in zip(shape[:0:-1], strides[:0:-1]):
+        together = together and (size == 1 or stride == n)
+        n *= size
+    if n != width or not together:
+        raise ValueError("rows of %d elements expected, heads back to back, not %s with strides %s" % (width, tuple(shape), strides))
+    return x.data_ptr(), strides[0] if shape[0] > 1 else width
+
+
+def _p(a):
+    """The elements of an int64 or int32 array, for the library; keeps the array.  (a.ctypes.data_as takes 2.5 us, of calls of 10 to 20.)"""
+    t = C.c_int64 if a.itemsize == 8 else C.c_int32
+    try:
+        return (t * len(a)).from_buffer(a)
+    except (TypeError, ValueError):                 # read-only or empty
+        return a.ctypes.data_as(C.POINTER(t))
 
 
 def _i64(a):
@@ -275,8 +291,7 @@ class Context:
     # ---- layers
     def _batch(self, seq_ids, q_lens, kv_before):
         s, q, b = _i64(seq_ids), _i32(q_lens), _i32(kv_before)
-        bt = _Batch(len(s), s.ctypes.data_as(C.POINTER(C.c_int64)), q.ctypes.data_as(C.POINTER(C.c_int32)),
-                    b.ctypes.data_as(C.POINTER(C.c_int32)))
+        bt = _Batch(len(s), _p(s), _p(q), _p(b))
         return bt, (s, q, b)
 
     def layer_prefill(self, desc, layer, phase, seq_ids, q_lens, kv_before, x_in, out, stream=0):
@@ -298,11 +313,11 @@ class Context:
     # ---- KV movement
     def kv_swap(self, desc, direction, seq_ids, stream=0):
         s = _i64(seq_ids)
-        self._ck(self.lib.ss_kv_swap(self.h, C.byref(desc), direction, s.ctypes.data_as(C.POINTER(C.c_int64)), len(s), stream))
+        self._ck(self.lib.ss_kv_swap(self.h, C.byref(desc), direction, _p(s), len(s), stream))
 
     def kv_reshard(self, src, dst, seq_ids, stream=0):
         s = _i64(seq_ids)
-        self._ck(self.lib.ss_kv_reshard(self.h, C.byref(src), C.byref(dst), s.ctypes.data_as(C.POINTER(C.c_int64)), len(s), stream))
+        self._ck(self.lib.ss_kv_reshard(self.h, C.byref(src), C.byref(dst), _p(s), len(s), stream))
 
     def sync(self):
         self._ck(self.lib.ss_sync(self.h))
@@ -315,20 +330,20 @@ class Context:
 
     def kv_free(self, desc, seq_ids):
         s = _i64(seq_ids)
-        self._ck(self.lib.ss_kv_free(self.h, C.byref(desc), s.ctypes.data_as(C.POINTER(C.c_int64)), len(s)))
+        self._ck(self.lib.ss_kv_free(self.h, C.byref(desc), _p(s), len(s)))
 
     def host_tier_release(self, seq_ids):
         s = _i64(seq_ids)
-        self._ck(self.lib.ss_host_tier_release(self.h, s.ctypes.data_as(C.POINTER(C.c_int64)), len(s)))
+        self._ck(self.lib.ss_host_tier_release(self.h, _p(s), len(s)))
 
     def kv_export_dev(self, desc, seq_ids, staging, stream=0):
         s = _i64(seq_ids)
-        self._ck(self.lib.ss_kv_export_dev(self.h, C.byref(desc), s.ctypes.data_as(C.POINTER(C.c_int64)), len(s), _ptr(staging), stream))
+        self._ck(self.lib.ss_kv_export_dev(self.h, C.byref(desc), _p(s), len(s), _ptr(staging), stream))
 
     def kv_import_dev(self, desc, seq_ids, lens, staging, stream=0):
         s, l = _i64(seq_ids), _i32(lens)
-        self._ck(self.lib.ss_kv_import_dev(self.h, C.byref(desc), s.ctypes.data_as(C.POINTER(C.c_int64)),
-                                           l.ctypes.data_as(C.POINTER(C.c_int32)), len(s), _ptr(staging), stream))
+        self._ck(self.lib.ss_kv_import_dev(self.h, C.byref(desc), _p(s),
+                                           _p(l), len(s), _ptr(staging), stream))
 
     # ---- caches in 8 bits
     def _heads(self, desc):
@@ -338,9 +353,8 @@ class Context:
     def _qkv(self, desc, q, k, v, tokens):
         n_q, n_kv = self._heads(desc)
         d = self.model.head_dim
-        code = {"torch.float32": SS_F32, "torch.bfloat16": SS_BF16, "torch.float16": SS_F16}
         for x in (q, k, v):
-            if x is not None and (x.shape[0] != tokens or code.get(str(x.dtype)) != self.model.dtype or x.device.index != self.runtime.device):
+            if x is not None and (x.shape[0] != tokens or _TYPES.get(str(x.dtype)) != self.model.dtype or x.device.index != self.runtime.device):
                 raise ValueError("%d tokens of the model's type on its device expected, not %s of %s on %s" %
                                  (tokens, tuple(x.shape), x.dtype, x.device))
         (qp, qs), (kp, ks), (vp, vs) = _rows(q, n_q * d), _rows(k, n_kv * d), _rows(v, n_kv * d)
@@ -375,14 +389,14 @@ class Context:
     def kv8_weights(self, desc, direction, seq_ids, buf, stream=0):
         """buf: float32 on the device, [sequence][layer][head][token] back to back."""
         s = _i64(seq_ids)
-        self._ck(self.lib.ss_kv8_weights(self.h, C.byref(desc), direction, s.ctypes.data_as(C.POINTER(C.c_int64)), len(s), _ptr(buf), stream))
+        self._ck(self.lib.ss_kv8_weights(self.h, C.byref(desc), direction, _p(s), len(s), _ptr(buf), stream))
 
     def kv8_evict(self, desc, seq_ids, keep, recent, stream=0):
         s, k = _i64(seq_ids), _i32(keep)
         if len(s) != len(k):
             raise ValueError("%d sequences, %d lengths to keep" % (len(s), len(k)))
-        self._ck(self.lib.ss_kv8_evict(self.h, C.byref(desc), s.ctypes.data_as(C.POINTER(C.c_int64)),
-                                       k.ctypes.data_as(C.POINTER(C.c_int32)), len(s), recent, stream))
+        self._ck(self.lib.ss_kv8_evict(self.h, C.byref(desc), _p(s),
+                                       _p(k), len(s), recent, stream))
 
     # ---- inspection
     def kv_page_table(self, desc, seq):
