@@ -851,13 +851,36 @@ __global__ __launch_bounds__(256) void attn8_join_kernel(const float* __restrict
     const float* sp = scratch + ((size_t)rec[5] * 256 + i) * (D + 4);
     float M = -INFINITY, den = 0.f;
     f32x4_t num = {0.f, 0.f, 0.f, 0.f};
-    for (int u = 0; u < rec[6]; ++u, sp += 256 * (D + 4)) {
-        const float m = sp[D], l = sp[D + 1];
-        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(sp + e);
-        const float mx = fmaxf(M, m), ref = mx == -INFINITY ? 0.f : mx, alpha = exp2_fast(M - ref), w = exp2_fast(m - ref);
+    const int parts = rec[6];
+    for (int i0 = 0; i0 < parts; i0 += 4) {                              // four are requested together
+        float m[4], l[4], mx = M;
+        f32x4_t v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float* p = sp + (size_t)(i0 + u < parts ? i0 + u : parts - 1) * 256 * (D + 4);
+            m[u] = p[D];
+            l[u] = p[D + 1];
+            v[u] = *reinterpret_cast<const f32x4_t*>(p + e);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (i0 + u >= parts) {                                       // repeated: weight 0 would not keep an infinite one out
+                m[u] = -INFINITY;
+                l[u] = 0.f;
+                v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            }
+            mx = fmaxf(mx, m[u]);
+        }
+        const float ref = mx == -INFINITY ? 0.f : mx, alpha = exp2_fast(M - ref);
         M = mx;
-        num = num * alpha + w * v;
-        den = den * alpha + w * l;
+        num *= alpha;
+        den *= alpha;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float w = exp2_fast(m[u] - ref);
+            num += w * v[u];
+            den += w * l[u];
+        }
     }
     *reinterpret_cast<uint2*>(out + ((int64_t)(rec[3] + row / G) * n_q + rec[1] * G + row % G) * D + e) =
         make_uint2(pack_bf16x2(num[0] / den, num[1] / den), pack_bf16x2(num[2] / den, num[3] / den));

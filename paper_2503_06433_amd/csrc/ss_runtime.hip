@@ -1125,9 +1125,10 @@ struct Image {
 // Many items: they are taken pair by pair, the longest sequence first, the last rows first, and cut into eight shares of equal cost, so
 // that those that read the same pages mostly share an L2.  Within a share each goes to the block with the least work so far.
 // Fewer than eight a block: what bounds the time is the block with the most tiles.  Items of more than 1.15 times the mean (and of more than
-// 1024 tokens) are cut into parts along the keys, and each goes to the block with the least work of all.  Chunks of 500 tokens behind
+// six tiles) are cut into parts along the keys, and each goes to the block with the least work of all.  Chunks of 500 tokens behind
 // 1000 - 6000, 32 heads, where the longest of 256 items is 1.8 times the mean: 203 us uncut, 158 + 5 cut so; half as long or
-// shorter, the parts' sums cost more than is won (+ 25 us).  The same with each kv head's items on one XCD took as long.
+// shorter, the parts' sums cost more than is won (+ 25 us).  The same with each kv head's items on one XCD took as long.  The six: a
+// prompt of 2000 on one kv head 73 us, with 16 instead 78, with 32 91; with two no less.
 struct Prefill8 {
     std::vector<int32_t> items, cuts;
     int stride = 0, blocks = 0, n_parts = 0;
@@ -1167,7 +1168,7 @@ void prefill8_items(ss_ctx* c, Shard* s, int n, const std::vector<int32_t>& cu, 
         }
     } least;
     if (items.size() < (size_t)8 * n_blocks) {
-        const int most = (int)std::max<int64_t>(16, (total * 23 + 20 * n_blocks - 1) / (20 * n_blocks));
+        const int most = (int)std::max<int64_t>(6, (total * 23 + 20 * n_blocks - 1) / (20 * n_blocks));
         std::vector<Item> pieces;
         for (const Item& it : items) {
             const int tiles = (it.pages + 3) / 4;
