@@ -1,5 +1,5 @@
 // Cache in 8 bits: what fills it, reads it back, keeps the accumulated attention weights and evicts by them.  Everything here moves
-// data: bound by HBM.  The arithmetic of a block (see Kv8Layer): A = max |v|, q = rint(v * 127 / A).  The product v * 127 is exact
+// data: bound by HBM (32 prompts of 512 - 4096 tokens on 8 heads written in 107 us, 4.3 TB/s, and read back in 82, 5.6 TB/s).  The arithmetic of a block (see Kv8Layer): A = max |v|, q = rint(v * 127 / A).  The product v * 127 is exact
 // for 16-bit v and the quotient is correctly rounded; a quotient of two numbers of up to 11 bits is never closer to half a
 // step than 2^-12 without being on it, the error of the fp32 quotient is at most 2^-18: q is the one of real arithmetic.  For 32-bit v
 // a quotient that close to half a step is formed again in 64 bits (25 bits decide there).
@@ -380,7 +380,8 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
 // Which tokens stay.  A block per (head, layer, sequence).  The key of the last token that stays among the older ones is found digit
 // by digit (four histograms of 256), then one ordered pass lists the positions: all above that key, and of those
 // equal to it the first ones.
-// Keys are read from the cache once, to LDS, those behind the EV_KEYS first ones for every pass again.
+// Keys are read from the cache once, to LDS, those behind the EV_KEYS first ones for every pass again.  256 lists of 1500 - 9000 keys: 22 us
+// (57 with keys read for every pass and the digit looked for by one lane).
 constexpr int EV_T = 1024, EV_KEYS = 36 * 1024;
 __global__ __launch_bounds__(EV_T) void kv8_select_kernel(const Kv8Layer* __restrict__ layers, int n_heads, Kv8Evict e, int32_t* __restrict__ lists) {
     __shared__ int hist[256], digit_s, left_s, eq_w[EV_T / 64], out_w[EV_T / 64];
@@ -469,7 +470,8 @@ __global__ __launch_bounds__(EV_T) void kv8_select_kernel(const Kv8Layer* __rest
 // page numbers one round and positions two rounds ahead.
 // A token's V is a byte of every row of its page: the page's rows are brought once, 16 bytes a lane, for all tokens that come from
 // it, and v_perm puts the bytes where they go (one load a token and row instead took twice the time).  Eight pages are requested ahead,
-// which is enough where half of a page or more stays; what lies behind them is waited for.
+// which is enough where half of a page or more stays; what lies behind them is waited for.  256 lists of 2048 tokens from up to 9000:
+// 130 us, 8 a round; with a wave a half of a block's elements and twice the waves 141, one load a byte 197.
 // In units of A / 127 the old values are q * A, exact in fp32 where A has the 16 bits of the model's type; those of the open
 // block are 127 * v.  The new block's magnitude in those units is W: A' = W / 127, q' = rint(value * 127 / W).  All in 32 bits,
 // for 32-bit models and blocks that were evicted before too, whose products are rounded.
