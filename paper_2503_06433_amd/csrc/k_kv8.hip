@@ -349,6 +349,76 @@ hipError_t kv8_rope(int dt, void* qkv, int n_q, int n_kv, int d, const float* ro
     return hipGetLastError();
 }
 
+// A decode step's one launch for both: queries rotated in place, the new token's key (rotated) and value into the open block, and that
+// quantised where it is full now.  One token a sequence, a unit of its own each.  A wave per (sequence, kv head), and one for every few query heads.
+// Rotation and write as two launches took 4 us more a layer, of 115 for eight sequences.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv8_step_kernel(T* __restrict__ qkv, int n_q, int n_kv, const float* __restrict__ rope, Kv8Batch b, Kv8Layer kv) {
+    constexpr int V = VecOf<T>::N, HALF = D / 2 / V, HEADS = 64 / HALF;  // 16-byte pieces of half a head; query heads of a wave
+    __shared__ uint32_t lds[4][kv8_vwords<D>];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = n_kv + (n_q + HEADS - 1) / HEADS;
+    const int64_t id = (int64_t)blockIdx.x * 4 + wave;
+    if (id >= (int64_t)b.n_seqs * per) return;
+    const int sq = (int)(id / per), part = (int)(id % per), pos0 = b.before[sq], slot0 = pos0 & 15;
+    T* row = qkv + (size_t)b.cu_q[sq] * (n_q + 2 * n_kv) * D;
+    const int c = lane % HALF * V;
+    auto rotated = [&](const T* head, vec16& lo, vec16& hi) {
+        const float* cs = rope + (size_t)b.pos[sq] * D + 2 * c;
+        float x[V], y[V], ox[V], oy[V];
+        unpack16<T>(*reinterpret_cast<const vec16*>(head + c), x);
+        unpack16<T>(*reinterpret_cast<const vec16*>(head + D / 2 + c), y);
+#pragma unroll
+        for (int j = 0; j < V; ++j) rope_rotate(x[j], y[j], cs[2 * j], cs[2 * j + 1], ox[j], oy[j]);
+        lo = pack16<T>(ox);
+        hi = pack16<T>(oy);
+    };
+    vec16 lo, hi;
+    if (part >= n_kv) {
+        const int a = (part - n_kv) * HEADS + lane / HALF;
+        if (a >= n_q) return;
+        T* head = row + (size_t)a * D;
+        rotated(head, lo, hi);
+        *reinterpret_cast<vec16*>(head + c) = lo;
+        *reinterpret_cast<vec16*>(head + D / 2 + c) = hi;
+        return;
+    }
+    const int g = part;
+    const T *k = row + (size_t)(n_q + g) * D, *v = row + (size_t)(n_q + n_kv + g) * D;
+    T* ko = (T*)kv.open + ((size_t)b.slot[sq] * 2 * n_kv + g) * 16 * D;
+    T* vo = ko + (size_t)n_kv * 16 * D;
+    const size_t page = (size_t)b.page_tables[(size_t)sq * b.pt_stride + pos0 / 16] * n_kv + g;
+    if (lane < HALF) {
+        rotated(k, lo, hi);
+        *reinterpret_cast<vec16*>(ko + slot0 * D + c) = lo;
+        *reinterpret_cast<vec16*>(ko + slot0 * D + D / 2 + c) = hi;
+    }
+    if (lane < 2 * HALF) *reinterpret_cast<vec16*>(vo + slot0 * D + lane * V) = *reinterpret_cast<const vec16*>(v + lane * V);
+    if (kv.w && lane == 0) kv.w[page * 16 + slot0] = 0.f;
+    if (slot0 == 15) {
+        __builtin_amdgcn_wave_barrier();
+        __threadfence_block();                                           // the rows that were just stored are read back by other lanes
+        Kv8Tile<T, D> tk, tv;
+        kv8_load_tile<T, D>(tk, nullptr, 0, ko, 16, lane);
+        kv8_load_tile<T, D>(tv, nullptr, 0, vo, 16, lane);
+        kv8_store_block<T, D>(tk, tv, kv.k + page * 16 * D, kv.v + page * 16 * D, kv.amax + page * 2, lds[wave], lane);
+    }
+}
+
+template <typename T, int D>
+static void launch_step(void* qkv, int n_q, int n_kv, const float* rope, const Kv8Batch& b, const Kv8Layer& kv, unsigned blocks, hipStream_t s) {
+    kv8_step_kernel<T, D><<<blocks, 256, 0, s>>>((T*)qkv, n_q, n_kv, rope, b, kv);
+}
+
+hipError_t kv8_step(int dt, void* qkv, int n_q, int n_kv, int d, const float* rope_table, const Kv8Batch& b, const Kv8Layer& kv, hipStream_t s) {
+    if (b.n_seqs <= 0) return hipSuccess;
+    if ((d != 64 && d != 128) || n_q <= 0 || n_kv <= 0 || b.max_q_len != 1 || b.n_units != b.n_seqs || (uintptr_t)qkv % 16) return hipErrorInvalidValue;
+    const int heads = 64 / (d / 2 / (dt == F32 ? 4 : 8));
+    const long long waves = (long long)b.n_seqs * (n_kv + (n_q + heads - 1) / heads);
+    if (waves > 0x7fffffffll) return hipErrorInvalidValue;
+    SS_TYPED(dt, d, launch_step, (qkv, n_q, n_kv, rope_table, b, kv, (unsigned)((waves + 3) / 4), s));
+    return hipGetLastError();
+}
+
 // ---------------------------------------------------------------- accumulated weights of whole sequences
 __global__ __launch_bounds__(256) void kv8_weights_kernel(const Kv8Layer* __restrict__ layers, int n_heads, RepackUnits u, float* __restrict__ buf,
                                                           bool in) {

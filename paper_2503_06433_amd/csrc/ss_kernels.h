@@ -275,6 +275,8 @@ hipError_t copy_elems(int dt, const void* src, void* dst, int64_t n, hipStream_t
 // ---- caches in 8 bits (Kv8Layer)
 // Rotates q and k in place inside qkv [T, (n_q + 2 n_kv) d].
 hipError_t kv8_rope(int dt, void* qkv, int n_q, int n_kv, int d, const float* rope_table, const Kv8Batch& b, hipStream_t s);
+// One token a sequence: rotates q in place and brings the rotated k and v into the cache.
+hipError_t kv8_step(int dt, void* qkv, int n_q, int n_kv, int d, const float* rope_table, const Kv8Batch& b, const Kv8Layer& kv, hipStream_t s);
 
 // The batch's new tokens into the cache.  k, v: rows of n_heads * d elements, `k_stride` / `v_stride` elements apart.
 hipError_t kv8_write(int dt, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int n_heads, int d, const Kv8Batch& b,

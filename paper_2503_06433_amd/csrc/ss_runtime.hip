@@ -1408,9 +1408,13 @@ int run_attn_phase8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode,
     const uint8_t* qkv = (const uint8_t*)c->ws_qkv.p;
     {
         ProfScope ps(c, 4, st);
-        K_TRY(c, SSK_CALL(c, kv8_rope, c->ws_qkv.p, s->nq_l, s->nkv_l, d, c->d_rope, ms->b, st));
-        K_TRY(c, SSK_CALL(c, kv8_write, qkv + (size_t)s->nq_l * d * c->es, nqkv, qkv + (size_t)(s->nq_l + s->nkv_l) * d * c->es, nqkv, s->nkv_l, d,
-                          ms->b, s->kv8_layers[ll], st));
+        if (decode) {
+            K_TRY(c, SSK_CALL(c, kv8_step, c->ws_qkv.p, s->nq_l, s->nkv_l, d, c->d_rope, ms->b, s->kv8_layers[ll], st));
+        } else {
+            K_TRY(c, SSK_CALL(c, kv8_rope, c->ws_qkv.p, s->nq_l, s->nkv_l, d, c->d_rope, ms->b, st));
+            K_TRY(c, SSK_CALL(c, kv8_write, qkv + (size_t)s->nq_l * d * c->es, nqkv, qkv + (size_t)(s->nq_l + s->nkv_l) * d * c->es, nqkv, s->nkv_l,
+                              d, ms->b, s->kv8_layers[ll], st));
+        }
     }
     if ((rc = run_attn8(c, s, ll, ms, decode, qkv, nqkv, c->ws_attn.p, st))) return rc;
     {
