@@ -139,3 +139,35 @@ def test_eviction_of_extreme_values(d):
         toks.append(tuple(pair))
     w = [rng.exponential(size=(2, n)).astype(np.float32) for n in lens]
     _evicted(c, toks, w, keep, 20)
+
+
+def test_pages_beyond_4_gb():
+    """The same calls in a small cache and in one whose first 65 600 pages (4.3 GB of K, as much of V) are taken: the same bits."""
+    rng = np.random.default_rng(36)
+    heads, d, n, taken = 32, 128, 1190, 65600
+    small = Cache(wl.BF16, heads, heads, d, pages=90, seqs=4, weights=True)
+    large = Cache(wl.BF16, heads, heads, d, pages=taken + 90, seqs=300, weights=True)
+    fill = torch.ones(16 * 4096, heads, d, device="cuda", dtype=torch.bfloat16)
+    left, first = taken, 1000
+    while left:
+        seqs = [min(256, left - 256 * i) for i in range(16) if left > 256 * i]                   # pages, 4096 tokens at most
+        t = 16 * sum(seqs)
+        large.ctx.kv8_write(large.desc, 0, list(range(first, first + len(seqs))), [16 * p for p in seqs], [0] * len(seqs), fill[:t], fill[:t])
+        left -= sum(seqs)
+        first += len(seqs)
+    del fill
+    q, k, v = (small.tokens(rng, n + 2, heads)[1] for _ in range(3))
+    res = []
+    for c in (small, large):
+        got = [attn(c, 0, [1], [n], [0], q[:n], k[:n], v[:n], False)]
+        got += [attn(c, 0, [1], None, [n + i], q[n + i:n + i + 1], k[n + i:n + i + 1], v[n + i:n + i + 1], True) for i in range(2)]
+        w = torch.full((heads * (n + 2),), -1.0, device="cuda")
+        c.ctx.kv8_weights(c.desc, ss.SS_OUT, [1], w)
+        got += [w.cpu().numpy(), c.export([1], [n + 2])[0]]
+        c.ctx.kv8_evict(c.desc, [1], [300], 30)
+        got.append(c.export([1], [300])[0])
+        res.append(got)
+    assert large.ctx.kv_page_table(large.desc, 1).min() >= taken
+    for a, b in zip(*res):
+        assert np.isfinite(a).all()
+        np.testing.assert_array_equal(a, b)
