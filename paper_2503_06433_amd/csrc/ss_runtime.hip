@@ -13,9 +13,11 @@
 #include <cstdlib>
 #include <cstring>
 #include <deque>
+#include <exception>
 #include <functional>
 #include <map>
 #include <mutex>
+#include <new>
 #include <queue>
 #include <string>
 #include <thread>
@@ -1060,6 +1062,18 @@ int run_attn_phase(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, 
 static int decode8_item_pages(int64_t total_pages, int n_kv_local) {
     const int64_t n = (total_pages * n_kv_local + 2047) / 2048;
     return (int)(std::max<int64_t>(8, std::min<int64_t>(256, n + 3)) & ~3);
+}
+
+// No exception leaves a C entry: lists of a batch that host memory does not hold are an error like any other.
+template <class F>
+int guarded(ss_ctx* c, F f) {
+    try {
+        return f();
+    } catch (const std::bad_alloc&) {
+        return fail(c, SS_ENOMEM, "out of host memory");
+    } catch (const std::exception& e) {
+        return fail(c, SS_EINVAL, "%s", e.what());
+    }
 }
 
 int refuse_capture(ss_ctx* c, hipStream_t st) {
@@ -2848,18 +2862,18 @@ int ss_kv8_enable(ss_ctx* c, const ss_shard_desc* d, const ss_kv8_cfg* cfg) {
 }
 
 int ss_kv8_write(ss_ctx* c, const ss_shard_desc* d, int layer, const ss_batch* b, const ss_qkv* x, void* stream) {
-    return kv8_call(c, d, layer, b, x, nullptr, stream, 0);
+    return guarded(c, [&] { return kv8_call(c, d, layer, b, x, nullptr, stream, 0); });
 }
 
 int ss_kv8_attn_prefill(ss_ctx* c, const ss_shard_desc* d, int layer, const ss_batch* b, const ss_qkv* x, void* out, void* stream) {
-    return kv8_call(c, d, layer, b, x, out, stream, 1);
+    return guarded(c, [&] { return kv8_call(c, d, layer, b, x, out, stream, 1); });
 }
 
 int ss_kv8_attn_decode(ss_ctx* c, const ss_shard_desc* d, int layer, const ss_batch* b, const ss_qkv* x, void* out, void* stream) {
-    return kv8_call(c, d, layer, b, x, out, stream, 2);
+    return guarded(c, [&] { return kv8_call(c, d, layer, b, x, out, stream, 2); });
 }
 
-int ss_kv8_weights(ss_ctx* c, const ss_shard_desc* d, int dir, const int64_t* seq_ids, int n, float* buf, void* stream) {
+static int kv8_weights_call(ss_ctx* c, const ss_shard_desc* d, int dir, const int64_t* seq_ids, int n, float* buf, void* stream) {
     if (!c) return SS_EINVAL;
     if (n < 0 || (n > 0 && (!seq_ids || !buf))) return fail(c, SS_EINVAL, "bad arguments");
     if (dir != SS_OUT && dir != SS_IN) return fail(c, SS_EINVAL, "bad direction %d", dir);
@@ -2887,7 +2901,7 @@ int ss_kv8_weights(ss_ctx* c, const ss_shard_desc* d, int dir, const int64_t* se
     });
 }
 
-int ss_kv8_evict(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, const int32_t* keep, int n, int recent, void* stream) {
+static int kv8_evict_call(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, const int32_t* keep, int n, int recent, void* stream) {
     if (!c) return SS_EINVAL;
     if (n < 0 || (n > 0 && (!seq_ids || !keep)) || recent < 0) return fail(c, SS_EINVAL, "bad arguments");
     DeviceScope dev(c->rt.device);
@@ -2959,6 +2973,14 @@ int ss_kv8_evict(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, cons
     }
     s->version++;
     return mark_meta8_used(c, ms, st);
+}
+
+int ss_kv8_weights(ss_ctx* c, const ss_shard_desc* d, int dir, const int64_t* seq_ids, int n, float* buf, void* stream) {
+    return guarded(c, [&] { return kv8_weights_call(c, d, dir, seq_ids, n, buf, stream); });
+}
+
+int ss_kv8_evict(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, const int32_t* keep, int n, int recent, void* stream) {
+    return guarded(c, [&] { return kv8_evict_call(c, d, seq_ids, keep, n, recent, stream); });
 }
 
 int ss_kv_page_table(ss_ctx* c, const ss_shard_desc* d, int64_t seq, int32_t* pages, int32_t* n_inout) {
