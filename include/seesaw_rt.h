@@ -261,7 +261,8 @@ int ss_kv_import_dev(ss_ctx*, const ss_shard_desc*, const int64_t* seq_ids, cons
  *   (A query that sees a value that is not finite in the open block has at least that element not finite, and may have
  *   NaN in the head's others; one that does not see it is not touched.)
  * ss_kv8_attn_decode: the same, one token per sequence, which adds the softmax weights of all query heads of a kv
- *   head to the weights of the tokens they fell on, if the shard keeps them (prefill does not).
+ *   head to the weights of the tokens they fell on, if the shard keeps them (prefill does not; a step that is repeated
+ *   adds them again).
  *   q, k, v: device, model dtype, 16-byte aligned; tokens *_stride elements apart (a multiple of 16 bytes), heads
  *   back to back, so that they may be parts of one fused row.  out must not overlap them.
  * ss_kv8_weights: the accumulated weights of whole sequences out of (SS_OUT) or into (SS_IN) buf, device,

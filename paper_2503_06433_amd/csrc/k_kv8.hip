@@ -395,8 +395,9 @@ __global__ __launch_bounds__(256) void kv8_step_kernel(T* __restrict__ qkv, int 
     if (lane < 2 * HALF) *reinterpret_cast<vec16*>(vo + slot0 * D + lane * V) = *reinterpret_cast<const vec16*>(v + lane * V);
     if (kv.w && lane == 0) kv.w[page * 16 + slot0] = 0.f;
     if (slot0 == 15) {
-        __builtin_amdgcn_wave_barrier();
-        __threadfence_block();                                           // the rows that were just stored are read back by other lanes
+        // the rows that were just stored are read back by other lanes of the wave
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __threadfence_block();
         Kv8Tile<T, D> tk, tv;
         kv8_load_tile<T, D>(tk, nullptr, 0, ko, 16, lane);
         kv8_load_tile<T, D>(tv, nullptr, 0, vo, 16, lane);
