@@ -170,18 +170,19 @@ __device__ __forceinline__ void v_step(float amax, float& lv, float& inv) {
 // 16 scores of page p, one query a lane: one K and one V step a lane, and 16-byte loads of 16 tokens (V) or 16 elements (K),
 // half a cache line a row.  K of the next four pages is requested behind the score products of these, V of these in front of them.
 // Bound by the page reads: 256 sequences of 512 - 2560 tokens on 32 heads 533 us, 6.0 TB/s; 1024 of 512 - 4096 on one head 122 us, 4.9 TB/s
-// (waves of a few hundred tokens each).  One sequence of 700 tokens: 9 us and 4 for the merge, the chain table -> page -> sums.
+// (waves of a few hundred tokens each).  One sequence of 700 tokens: 8 us and 4 for the merge, the chain item -> pages -> sums.
 template <int D, bool WEIGHTS>
 __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restrict__ q, int64_t q_stride, int n_q, int n_kv, int n_ct,
                                                           Kv8Batch b, Kv8Layer kv, float* __restrict__ scratch, float* __restrict__ scores,
                                                           float scale_log2e) {
     constexpr int HB = D / 64, DT = D / 16;
     const int heads = n_kv * n_ct;
-    const int item = b.wk.item_order[blockIdx.x / heads], g = blockIdx.x % heads / n_ct, ct = blockIdx.x % n_ct;
+    const int32_t* rec = b.items + (size_t)(blockIdx.x / heads) * 8;
+    const int item = rec[0], g = blockIdx.x % heads / n_ct, ct = blockIdx.x % n_ct;
     const int G = n_q / n_kv;
-    const int sq = b.wk.item_seq[item], page0 = b.wk.item_page0[item], np = b.wk.item_npages[item];
+    const int sq = rec[1], page0 = rec[2], np = rec[3];
     const int npg = np & 0xffff, stride = (int)((unsigned)np >> 16);
-    const int p = b.before[sq], full = b.end[sq] / 16;
+    const int p = rec[4], full = rec[5] / 16, slot = rec[6], row = rec[7];
     const int lane = threadIdx.x, lq = lane & 15, g4 = lane >> 4;
     const bool open_here = page0 + (npg - 1) * stride >= full;           // the item's last page is the open block
     const int npc = npg - open_here;
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             qf[h][j].w[0] = qf[h][j].w[1] = qf[h][j].w[2] = qf[h][j].w[3] = 0u;
-            if (mine) qf[h][j].q = *reinterpret_cast<const vec16*>(q + (int64_t)b.cu_q[sq] * q_stride + (size_t)a * D + 64 * h + 16 * g4 + 8 * j);
+            if (mine) qf[h][j].q = *reinterpret_cast<const vec16*>(q + (int64_t)row * q_stride + (size_t)a * D + 64 * h + 16 * g4 + 8 * j);
         }
     f32x4_t o[DT];
 #pragma unroll
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
         // Tokens 4 g4 + v of the open block, in the model's type, in the first four of the group's eight slots of the second product.  V is
         // scaled by a power of two (exact) to below 128, as the whole numbers of a full block are.
         const int cnt = p - full * 16 + 1;
-        const bf16_t* ko = (const bf16_t*)kv.open + ((size_t)b.slot[sq] * 2 * n_kv + g) * 16 * D;
+        const bf16_t* ko = (const bf16_t*)kv.open + ((size_t)slot * 2 * n_kv + g) * 16 * D;
         const bf16_t* vo = ko + (size_t)n_kv * 16 * D;
         bf16_t raw[DT][4];
 #pragma unroll
@@ -391,7 +392,7 @@ __global__ __launch_bounds__(256) void attn8_merge_kernel(const float* __restric
     const int sq = blockIdx.y, e = threadIdx.x % (D / 4) * 4, row = threadIdx.x / (D / 4);
     const int a = SPLIT > 1 ? blockIdx.x : blockIdx.x * ROWS + row, step = SPLIT > 1 ? 4 * SPLIT : 4;
     if (a >= n_q) return;
-    const int i0 = b.wk.seq_item0[sq] + (SPLIT > 1 ? row * 4 : 0), i1 = b.wk.seq_item0[sq + 1];
+    const int i0 = b.seq_item0[sq] + (SPLIT > 1 ? row * 4 : 0), i1 = b.seq_item0[sq + 1];
     float M = -INFINITY, den = 0.f;
     f32x4_t num = {0.f, 0.f, 0.f, 0.f};
     for (int i = i0; i < i1; i += step) {
@@ -457,11 +458,11 @@ static void launch_decode(const void* q, int64_t q_stride, void* out, int n_q, i
                           float* scores, float* lse, hipStream_t s) {
     const int n_ct = (n_q / n_kv + 15) / 16;
     const float sl2 = 1.4426950408889634f / sqrtf((float)D);
-    const unsigned grid = (unsigned)((long long)b.wk.n_items * n_kv * n_ct);
+    const unsigned grid = (unsigned)((long long)b.n_items * n_kv * n_ct);
     const auto kernel = scores ? attn8_decode_kernel<D, true> : attn8_decode_kernel<D, false>;
     kernel<<<grid, 64, 0, s>>>((const bf16_t*)q, q_stride, n_q, n_kv, n_ct, b, kv, scratch, scores, sl2);
     constexpr int ROWS = 1024 / D;
-    if (b.wk.max_items_per_seq > ROWS) attn8_merge_kernel<D, ROWS><<<dim3(n_q, b.n_seqs), 256, 0, s>>>(scratch, (bf16_t*)out, n_q, b, lse);
+    if (b.max_items_per_seq > ROWS) attn8_merge_kernel<D, ROWS><<<dim3(n_q, b.n_seqs), 256, 0, s>>>(scratch, (bf16_t*)out, n_q, b, lse);
     else attn8_merge_kernel<D, 1><<<dim3((n_q + ROWS - 1) / ROWS, b.n_seqs), 256, 0, s>>>(scratch, (bf16_t*)out, n_q, b, lse);
 }
 
@@ -938,7 +939,7 @@ __global__ __launch_bounds__(256) void attn8_weights_kernel(const float* __restr
 }
 
 // partial results [n_items][n_q][d + 4], then (weights) the scores [pages seen][n_q][16] and the logarithms [n_seqs][n_q]
-static size_t partial_floats(const Kv8Batch& b, int n_q, int d) { return (size_t)b.wk.n_items * n_q * (d + 4); }
+static size_t partial_floats(const Kv8Batch& b, int n_q, int d) { return (size_t)b.n_items * n_q * (d + 4); }
 size_t attn8_decode_scratch_floats(const Kv8Batch& b, int n_q, int d, bool weights) {
     return partial_floats(b, n_q, d) + (weights ? (size_t)b.n_seqs * n_q + (size_t)b.seen_pages * n_q * 16 : 0);
 }
@@ -954,7 +955,7 @@ hipError_t attn8_decode(int dt, const void* q, int64_t q_stride, void* out, int 
     if (dt == F32 || force_generic) {
         e = attn8_generic(dt, q, q_stride, out, n_q, n_kv, d, b, kv, scores, lse, s);
     } else {
-        if (b.wk.n_items <= 0 || (long long)b.wk.n_items * n_kv * ((n_q / n_kv + 15) / 16) > 0x7fffffffll) return hipErrorInvalidValue;
+        if (b.n_items <= 0 || (long long)b.n_items * n_kv * ((n_q / n_kv + 15) / 16) > 0x7fffffffll) return hipErrorInvalidValue;
         if (d == 64) launch_decode<64>(q, q_stride, out, n_q, n_kv, b, kv, scratch, scores, lse, s);
         else launch_decode<128>(q, q_stride, out, n_q, n_kv, b, kv, scratch, scores, lse, s);
         e = hipGetLastError();

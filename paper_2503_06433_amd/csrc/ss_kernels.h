@@ -145,7 +145,11 @@ struct Kv8Batch {
     int pf_stride, pf_blocks;
     const int32_t* pf_cuts;
     int n_cuts, n_parts;
-    DecodeWork wk;               // pages include the open block's
+    // decode: 8 numbers an item, longest first: (its number, sequence, first page, pages | stride << 16, before, end, slot, cu_q); pages
+    // include the open block's.  Items are numbered sequence by sequence.
+    const int32_t* items;
+    const int32_t* seq_item0;    // [n_seqs + 1]
+    int n_items, max_items_per_seq;
 };
 
 // Sequences of an eviction (device arrays).

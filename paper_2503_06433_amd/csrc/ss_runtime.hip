@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <array>
 #include <atomic>
 #include <chrono>
 #include <condition_variable>
@@ -1333,34 +1334,31 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
             unit_cnt.push_back(p1 - p0);
         }
     // near-equal items of a sequence, interleaved: item j takes the pages j, j + cnt, ...
-    std::vector<int32_t> item_seq, item_page0, item_np, seq_item0, item_order;
-    int max_items = 0;
+    std::vector<int32_t> items, seq_item0;
+    int n_items = 0, max_items = 0;
     if (decode) {
         int64_t total_pages = 0;
         for (int i = 0; i < n; ++i) total_pages += before[i] / ps + 1;
         const int ipp = decode8_item_pages(total_pages, s->nkv_l);
+        std::vector<std::array<int32_t, 8>> recs;
         for (int i = 0; i < n; ++i) {
-            seq_item0.push_back((int32_t)item_seq.size());
+            seq_item0.push_back(n_items);
             const int used = before[i] / ps + 1, cnt = std::min((used + ipp - 1) / ipp, 65535);
-            for (int j = 0; j < cnt; ++j) {
-                item_seq.push_back(i);
-                item_page0.push_back(j);
-                item_np.push_back(((used - j + cnt - 1) / cnt) | (int)((unsigned)cnt << 16));
-            }
+            for (int j = 0; j < cnt; ++j)
+                recs.push_back({n_items++, i, j, ((used - j + cnt - 1) / cnt) | (int)((unsigned)cnt << 16), before[i], end[i], slot[i], cu[i]});
             max_items = std::max(max_items, cnt);
         }
-        seq_item0.push_back((int32_t)item_seq.size());
-        item_order.resize(item_seq.size());
-        for (size_t i = 0; i < item_order.size(); ++i) item_order[i] = (int32_t)i;
-        std::stable_sort(item_order.begin(), item_order.end(), [&](int32_t x, int32_t y) { return (item_np[x] & 0xffff) > (item_np[y] & 0xffff); });
+        seq_item0.push_back(n_items);
+        std::stable_sort(recs.begin(), recs.end(), [](const auto& x, const auto& y) { return (x[3] & 0xffff) > (y[3] & 0xffff); });
+        items.reserve(recs.size() * 8);
+        for (const auto& r : recs) items.insert(items.end(), r.begin(), r.end());
     }
     Prefill8 pf;
     if (!decode && c->dt != SS_F32) prefill8_items(c, s, n, cu, before, end, &pf);
     Image im;
     const size_t o_cu = im.add(cu), o_before = im.add(before), o_end = im.add(end), o_slot = im.add(slot), o_pos = im.add(pos),
                  o_tok = im.add(pg_off), o_pt = im.add(pt), o_us = im.add(unit_seq), o_ut = im.add(unit_tok0), o_up = im.add(unit_pos0),
-                 o_uc = im.add(unit_cnt), o_is = im.add(item_seq), o_ip = im.add(item_page0), o_in = im.add(item_np), o_si = im.add(seq_item0),
-                 o_io = im.add(item_order), o_pf = im.add(pf.items), o_pc = im.add(pf.cuts);
+                 o_uc = im.add(unit_cnt), o_it = im.add(items), o_si = im.add(seq_item0), o_pf = im.add(pf.items), o_pc = im.add(pf.cuts);
     Meta8Slot* ms = nullptr;
     int rc = meta8_slot(c, im.total, &ms);
     if (rc) return rc;
@@ -1374,8 +1372,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
     k.unit_seq = at(o_us); k.unit_tok0 = at(o_ut); k.unit_pos0 = at(o_up); k.unit_cnt = at(o_uc); k.n_units = (int)unit_seq.size();
     k.pf_items = pf.items.empty() ? nullptr : at(o_pf); k.pf_stride = pf.stride; k.pf_blocks = pf.blocks;
     k.pf_cuts = at(o_pc); k.n_cuts = (int)pf.cuts.size() / 8; k.n_parts = pf.n_parts;
-    k.wk.item_seq = at(o_is); k.wk.item_page0 = at(o_ip); k.wk.item_npages = at(o_in); k.wk.seq_item0 = at(o_si); k.wk.item_order = at(o_io);
-    k.wk.n_items = (int)item_seq.size(); k.wk.max_items_per_seq = max_items;
+    k.items = at(o_it); k.seq_item0 = at(o_si); k.n_items = n_items; k.max_items_per_seq = max_items;
     ms->shard = s; ms->version = s->version; ms->decode = decode; ms->write = write;
     ms->seq_ids.assign(b->seq_ids, b->seq_ids + n);
     ms->q_lens.assign(b->q_lens, b->q_lens + n);
