@@ -1290,9 +1290,9 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
         return fail(c, SS_ENOMEM, "page pool exhausted: the batch needs %zu more pages, %zu free", more, s->free_pages.size());
     if (fresh > s->free_slots.size())
         return fail(c, SS_ENOMEM, "%zu new sequences, %zu of %d left in the cache in 8 bits", fresh, s->free_slots.size(), s->kv8_slots);
+    // a swap-out that has not run yet reads the open blocks, a swap-in the tokens wait for
+    wait_seqs_idle(c, s, b->seq_ids, n);
     if (write) {
-        // a swap-out that has not run yet reads the open blocks
-        wait_seqs_idle(c, s, b->seq_ids, n);
         for (int i = 0; i < n; ++i) {
             int rc = ensure_pages(c, s, b->seq_ids[i], end[i]);
             if (rc) return rc;
