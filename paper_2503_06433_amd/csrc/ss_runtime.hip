@@ -433,12 +433,15 @@ int fail(ss_ctx* c, int code, const char* fmt, ...) {
     return code;
 }
 
+// An error that is reported here is taken from the runtime: the next launch would find it there and fail with it.
 #define HIP_TRY(c, expr)                                                                        \
     do {                                                                                        \
         hipError_t e_ = (expr);                                                                 \
-        if (e_ != hipSuccess)                                                                   \
+        if (e_ != hipSuccess) {                                                                 \
+            (void)hipGetLastError();                                                            \
             return fail((c), e_ == hipErrorOutOfMemory ? SS_ENOMEM : SS_EHIP, "%s: %s (%s:%d)", #expr, \
                         hipGetErrorString(e_), __FILE__, __LINE__);                             \
+        }                                                                                       \
     } while (0)
 
 struct ProfScope {
