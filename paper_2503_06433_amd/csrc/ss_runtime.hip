@@ -135,7 +135,7 @@ struct Meta8Slot {
     // cache key
     Shard* shard = nullptr;
     uint64_t version = 0;
-    bool decode = false, write = false;
+    bool decode = false, write = false, attend = false;
     std::vector<int64_t> seq_ids;
     std::vector<int32_t> q_lens, before, end, pos;
     ssk::Kv8Batch b{};
@@ -1236,8 +1236,8 @@ void prefill8_items(ss_ctx* c, Shard* s, int n, const std::vector<int32_t>& cu, 
 }
 
 // Checks a batch over a cache in 8 bits, takes the pages of what it brings, builds (or finds) its metadata.  Nothing is changed unless
-// everything fits.
-int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool write, Meta8Slot** out) {
+// everything fits.  What only writes needs no work lists of attention and has none of its limits.
+int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool write, bool attend, Meta8Slot** out) {
     const int n = b->n_seqs, ps = 16;
     std::vector<int32_t> before(n), end(n), slot(n), pos(n);
     int64_t T = 0, seen = 0;
@@ -1287,7 +1287,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
         if (!s->seqs.count(b->seq_ids[i]))
             for (int j = 0; j < i; ++j)
                 if (b->seq_ids[j] == b->seq_ids[i]) return fail(c, SS_EINVAL, "sequence %lld is listed twice", (long long)b->seq_ids[i]);
-    if (T > (1 << 30) || (int64_t)max_q * (s->nq_l / s->nkv_l) > (1 << 30)) return fail(c, SS_EINVAL, "batch too large");
+    if (T > (1 << 30) || (attend && (int64_t)max_q * (s->nq_l / s->nkv_l) > (1 << 30))) return fail(c, SS_EINVAL, "batch too large");
     if (decode && s->kv8_weights && seen > INT32_MAX) return fail(c, SS_EINVAL, "batch too large: it sees %lld pages", (long long)seen);
     if (more > s->free_pages.size())
         return fail(c, SS_ENOMEM, "page pool exhausted: the batch needs %zu more pages, %zu free", more, s->free_pages.size());
@@ -1305,7 +1305,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
         }
     }
     for (auto& ms : c->meta8)
-        if (ms.shard == s && ms.version == s->version && ms.decode == decode && ms.write == write && (int)ms.seq_ids.size() == n &&
+        if (ms.shard == s && ms.version == s->version && ms.decode == decode && ms.write == write && ms.attend >= attend && (int)ms.seq_ids.size() == n &&
             std::equal(ms.seq_ids.begin(), ms.seq_ids.end(), b->seq_ids) && std::equal(ms.q_lens.begin(), ms.q_lens.end(), b->q_lens) &&
             ms.before == before && ms.end == end && ms.pos == pos) {
             *out = &ms;
@@ -1357,7 +1357,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
         for (const auto& r : recs) items.insert(items.end(), r.begin(), r.end());
     }
     Prefill8 pf;
-    if (!decode && c->dt != SS_F32) prefill8_items(c, s, n, cu, before, end, &pf);
+    if (attend && !decode && c->dt != SS_F32) prefill8_items(c, s, n, cu, before, end, &pf);
     Image im;
     const size_t o_cu = im.add(cu), o_before = im.add(before), o_end = im.add(end), o_slot = im.add(slot), o_pos = im.add(pos),
                  o_tok = im.add(pg_off), o_pt = im.add(pt), o_us = im.add(unit_seq), o_ut = im.add(unit_tok0), o_up = im.add(unit_pos0),
@@ -1376,7 +1376,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
     k.pf_items = pf.items.empty() ? nullptr : at(o_pf); k.pf_stride = pf.stride; k.pf_blocks = pf.blocks;
     k.pf_cuts = at(o_pc); k.n_cuts = (int)pf.cuts.size() / 8; k.n_parts = pf.n_parts;
     k.items = at(o_it); k.seq_item0 = at(o_si); k.n_items = n_items; k.max_items_per_seq = max_items;
-    ms->shard = s; ms->version = s->version; ms->decode = decode; ms->write = write;
+    ms->shard = s; ms->version = s->version; ms->decode = decode; ms->write = write; ms->attend = attend;
     ms->seq_ids.assign(b->seq_ids, b->seq_ids + n);
     ms->q_lens.assign(b->q_lens, b->q_lens + n);
     ms->before = std::move(before); ms->end = std::move(end); ms->pos = std::move(pos);
@@ -1408,7 +1408,7 @@ int run_attn_phase8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode,
     int rc = refuse_capture(c, st);
     if (rc) return rc;
     Meta8Slot* ms = nullptr;
-    if ((rc = prepare8(c, s, ll, b, decode, true, &ms))) return rc;
+    if ((rc = prepare8(c, s, ll, b, decode, true, true, &ms))) return rc;
     const int T = ms->b.T, H = m.hidden, d = m.head_dim;
     const int nqkv = (s->nq_l + 2 * s->nkv_l) * d;
     const size_t qkv_bytes = align256((size_t)T * nqkv * c->es);
@@ -2833,7 +2833,7 @@ int kv8_call(ss_ctx* c, const ss_shard_desc* d, int layer, const ss_batch* b, co
     if ((rc = ensure_pools(c, s))) return rc;
     Meta8Slot* ms = nullptr;
     const int ll = layer - d->layer_begin;
-    if ((rc = prepare8(c, s, ll, b, what == 2, write, &ms))) return rc;
+    if ((rc = prepare8(c, s, ll, b, what == 2, write, what != 0, &ms))) return rc;
     if (ms->pending) {
         HIP_TRY(c, ssk::upload(ms->job.src, ms->job.dst, (size_t)ms->job.n16 * 16, st));
         ms->pending = false;
