@@ -251,7 +251,8 @@ int ss_kv_import_dev(ss_ctx*, const ss_shard_desc*, const int64_t* seq_ids, cons
  * be the layer's number of tokens of that sequence, or to cut the cache back: to a multiple of 16, or to a place inside
  * the block its last tokens went to (a step may be repeated); SS_EINVAL otherwise.  A sequence is listed once per batch.
  * Calls on a capturing stream are refused (SS_EHIP): a graph would hold the page lists of now.  They wait on
- * the host for queued movements of their sequences.
+ * the host for queued movements of their sequences.  A call that is refused, or finds no memory, leaves the cache as it was.
+ * Attention takes up to 65535 sequences a batch.
  *
  * ss_kv8_write: the batch's keys and values, already rotated, into `layer` of the cache.
  * ss_kv8_attn_prefill: writes qkv->k and qkv->v like ss_kv8_write, then out [T, n_q * head_dim] = causal attention of

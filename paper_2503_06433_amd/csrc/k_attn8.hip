@@ -904,6 +904,12 @@ static hipError_t launch_prefill(const void* q, int64_t q_stride, void* out, int
 
 size_t attn8_prefill_scratch_floats(const Kv8Batch& b, int d) { return (size_t)b.n_parts * 256 * (d + 4); }
 
+bool attn8_takes(int dt, int n_q, int n_kv, int d, const Kv8Batch& b, bool decode, bool force_generic) {
+    if (!attn8_fits(n_q, n_kv, d, b, nullptr, 0, dt)) return false;
+    if (!decode) return true;
+    return (long long)b.max_seen * n_kv <= 0x7fffff00ll && (dt == F32 || force_generic || (long long)b.n_items * n_kv * ((n_q / n_kv + 15) / 16) <= 0x7fffffffll);
+}
+
 hipError_t attn8_prefill(int dt, const void* q, int64_t q_stride, void* out, int n_q, int n_kv, int d, const Kv8Batch& b,
                          const Kv8Layer& kv, float* scratch, bool force_generic, hipStream_t s) {
     if (b.T <= 0 || b.n_seqs <= 0) return hipSuccess;
@@ -947,15 +953,15 @@ size_t attn8_decode_scratch_floats(const Kv8Batch& b, int n_q, int d, bool weigh
 hipError_t attn8_decode(int dt, const void* q, int64_t q_stride, void* out, int n_q, int n_kv, int d, const Kv8Batch& b,
                         const Kv8Layer& kv, float* scratch, bool force_generic, hipStream_t s) {
     if (b.n_seqs <= 0) return hipSuccess;
-    if (!attn8_fits(n_q, n_kv, d, b, q, q_stride, dt) || b.max_q_len != 1 || !scratch) return hipErrorInvalidValue;
-    if ((long long)b.max_seen * n_kv > 0x7fffff00ll) return hipErrorInvalidValue;
+    if (!attn8_fits(n_q, n_kv, d, b, q, q_stride, dt) || b.max_q_len != 1 || !scratch || !attn8_takes(dt, n_q, n_kv, d, b, true, force_generic))
+        return hipErrorInvalidValue;
     float* scores = kv.w ? scratch + partial_floats(b, n_q, d) : nullptr;
     float* lse = kv.w ? scores + (size_t)b.seen_pages * n_q * 16 : nullptr;
     hipError_t e = hipSuccess;
     if (dt == F32 || force_generic) {
         e = attn8_generic(dt, q, q_stride, out, n_q, n_kv, d, b, kv, scores, lse, s);
     } else {
-        if (b.n_items <= 0 || (long long)b.n_items * n_kv * ((n_q / n_kv + 15) / 16) > 0x7fffffffll) return hipErrorInvalidValue;
+        if (b.n_items <= 0) return hipErrorInvalidValue;
         if (d == 64) launch_decode<64>(q, q_stride, out, n_q, n_kv, b, kv, scratch, scores, lse, s);
         else launch_decode<128>(q, q_stride, out, n_q, n_kv, b, kv, scratch, scores, lse, s);
         e = hipGetLastError();

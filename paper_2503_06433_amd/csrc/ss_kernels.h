@@ -300,6 +300,8 @@ hipError_t kv8_evict(int dt, const Kv8Layer* layers, int n_heads, int d, const K
 hipError_t attn8_prefill(int dt, const void* q, int64_t q_stride, void* out, int n_q, int n_kv, int d, const Kv8Batch& b,
                          const Kv8Layer& kv, float* scratch, bool force_generic, hipStream_t s);
 size_t attn8_prefill_scratch_floats(const Kv8Batch& b, int d);
+// Whether the attention of a batch can be launched (the alignment of its queries aside).
+bool attn8_takes(int dt, int n_q, int n_kv, int d, const Kv8Batch& b, bool decode, bool force_generic);
 
 // One query per sequence.  With kv.w the weights of all query heads are added to it.  scratch: attn8_decode_scratch_floats.
 size_t attn8_decode_scratch_floats(const Kv8Batch& b, int n_q, int d, bool weights);

@@ -1109,6 +1109,7 @@ int meta8_slot(ss_ctx* c, size_t total, Meta8Slot** out) {
     }
     void* mapped = nullptr;
     HIP_TRY(c, hipHostGetDevicePointer(&mapped, ms.host, 0));
+    if (!ms.done) HIP_TRY(c, hipEventCreateWithFlags(&ms.done, hipEventDisableTiming));
     ms.job = {mapped, ms.dev, (int64_t)((total + 15) / 16)};
     ms.pending = true;
     *out = &ms;
@@ -1235,9 +1236,33 @@ void prefill8_items(ss_ctx* c, Shard* s, int n, const std::vector<int32_t>& cu, 
         }
 }
 
-// Checks a batch over a cache in 8 bits, takes the pages of what it brings, builds (or finds) its metadata.  Nothing is changed unless
-// everything fits.  What only writes needs no work lists of attention and has none of its limits.
-int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool write, bool attend, Meta8Slot** out) {
+// What a batch has taken of a shard while it is not certain yet that its tokens are written: pages, open blocks, new sequences.  Given
+// back unless it is kept.
+struct Taken8 {
+    Shard* s = nullptr;
+    struct Was { int64_t seq; bool fresh; size_t pages; int32_t len; };
+    std::vector<Was> was;
+    void keep() { s = nullptr; }
+    ~Taken8() {
+        if (!s || was.empty()) return;
+        for (auto w = was.rbegin(); w != was.rend(); ++w) {
+            auto it = s->seqs.find(w->seq);
+            if (it == s->seqs.end()) continue;
+            SeqState& st = it->second;
+            for (; st.pages.size() > w->pages; st.pages.pop_back()) s->free_pages.push(st.pages.back());
+            st.len = w->len;
+            if (!w->fresh) continue;
+            if (st.slot >= 0) s->free_slots.push(st.slot);
+            s->seqs.erase(it);
+        }
+        s->version++;
+    }
+};
+
+// Checks a batch over a cache in 8 bits, takes the pages of what it brings, builds (or finds) its metadata.  What it takes is in `taken`;
+// the layer's number of tokens changes only with kv8_written.  What only writes needs no work lists of attention and has none of its
+// limits.
+int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool write, bool attend, Taken8* taken, Meta8Slot** out) {
     const int n = b->n_seqs, ps = 16;
     std::vector<int32_t> before(n), end(n), slot(n), pos(n);
     int64_t T = 0, seen = 0;
@@ -1288,6 +1313,7 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
             for (int j = 0; j < i; ++j)
                 if (b->seq_ids[j] == b->seq_ids[i]) return fail(c, SS_EINVAL, "sequence %lld is listed twice", (long long)b->seq_ids[i]);
     if (T > (1 << 30) || (attend && (int64_t)max_q * (s->nq_l / s->nkv_l) > (1 << 30))) return fail(c, SS_EINVAL, "batch too large");
+    if (attend && (n > 65535 || s->nq_l > 65535)) return fail(c, SS_EINVAL, "batch too large: %d sequences, %d query heads", n, s->nq_l);
     if (decode && s->kv8_weights && seen > INT32_MAX) return fail(c, SS_EINVAL, "batch too large: it sees %lld pages", (long long)seen);
     if (more > s->free_pages.size())
         return fail(c, SS_ENOMEM, "page pool exhausted: the batch needs %zu more pages, %zu free", more, s->free_pages.size());
@@ -1296,12 +1322,14 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
     // a swap-out that has not run yet reads the open blocks, a swap-in the tokens wait for
     wait_seqs_idle(c, s, b->seq_ids, n);
     if (write) {
+        taken->was.reserve(n);
+        taken->s = s;
         for (int i = 0; i < n; ++i) {
+            auto it = s->seqs.find(b->seq_ids[i]);
+            const bool is_new = it == s->seqs.end();
+            taken->was.push_back({b->seq_ids[i], is_new, is_new ? 0 : it->second.pages.size(), is_new ? 0 : it->second.len});
             int rc = ensure_pages(c, s, b->seq_ids[i], end[i]);
             if (rc) return rc;
-            SeqState& st = s->seqs[b->seq_ids[i]];
-            st.layer_len[ll] = end[i];
-            st.len = *std::max_element(st.layer_len.begin(), st.layer_len.end());
         }
     }
     for (auto& ms : c->meta8)
@@ -1384,18 +1412,33 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
     return SS_OK;
 }
 
+// The batch's tokens are in the layer: its lengths, and what it took stays taken.
+void kv8_written(Shard* s, int ll, const Meta8Slot* ms, Taken8* taken) {
+    taken->keep();
+    for (size_t i = 0; i < ms->seq_ids.size(); ++i) {
+        SeqState& st = s->seqs.find(ms->seq_ids[i])->second;
+        st.layer_len[ll] = ms->end[i];
+        st.len = *std::max_element(st.layer_len.begin(), st.layer_len.end());
+    }
+}
+
+// What the batch's attention needs besides its metadata, before anything is written: behind the write it finds no reason to fail.
+int attn8_ready(ss_ctx* c, Shard* s, const Meta8Slot* ms, bool decode) {
+    const int d = c->m.head_dim;
+    if (!SSK_CALL(c, attn8_takes, s->nq_l, s->nkv_l, d, ms->b, decode, c->force_generic))
+        return fail(c, SS_EINVAL, "batch too large for the attention kernels");
+    if (!decode) return ms->b.n_parts ? ensure_buf(c, c->ws_scratch, sizeof(float) * ssk::attn8_prefill_scratch_floats(ms->b, d)) : SS_OK;
+    return ensure_buf(c, c->ws_scratch, sizeof(float) * ssk::attn8_decode_scratch_floats(ms->b, s->nq_l, d, s->kv8_weights));
+}
+
 int run_attn8(ss_ctx* c, Shard* s, int ll, Meta8Slot* ms, bool decode, const void* q, int64_t q_stride, void* out, hipStream_t st) {
     const int d = c->m.head_dim;
     const ssk::Kv8Layer& kv = s->kv8_layers[ll];
     if (!decode) {
-        const int rc = ms->b.n_parts ? ensure_buf(c, c->ws_scratch, sizeof(float) * ssk::attn8_prefill_scratch_floats(ms->b, d)) : SS_OK;
-        if (rc) return rc;
         ProfScope ps(c, 1, st);
         K_TRY(c, SSK_CALL(c, attn8_prefill, q, q_stride, out, s->nq_l, s->nkv_l, d, ms->b, kv, (float*)c->ws_scratch.p, c->force_generic, st));
         return SS_OK;
     }
-    const int rc = ensure_buf(c, c->ws_scratch, sizeof(float) * ssk::attn8_decode_scratch_floats(ms->b, s->nq_l, d, s->kv8_weights));
-    if (rc) return rc;
     ProfScope ps(c, 2, st);
     K_TRY(c, SSK_CALL(c, attn8_decode, q, q_stride, out, s->nq_l, s->nkv_l, d, ms->b, kv, (float*)c->ws_scratch.p, c->force_generic, st));
     return SS_OK;
@@ -1407,8 +1450,9 @@ int run_attn_phase8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode,
     const LayerW& w = s->w[ll];
     int rc = refuse_capture(c, st);
     if (rc) return rc;
+    Taken8 taken;
     Meta8Slot* ms = nullptr;
-    if ((rc = prepare8(c, s, ll, b, decode, true, true, &ms))) return rc;
+    if ((rc = prepare8(c, s, ll, b, decode, true, true, &taken, &ms)) || (rc = attn8_ready(c, s, ms, decode))) return rc;
     const int T = ms->b.T, H = m.hidden, d = m.head_dim;
     const int nqkv = (s->nq_l + 2 * s->nkv_l) * d;
     const size_t qkv_bytes = align256((size_t)T * nqkv * c->es);
@@ -1430,6 +1474,7 @@ int run_attn_phase8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode,
                               d, ms->b, s->kv8_layers[ll], st));
         }
     }
+    kv8_written(s, ll, ms, &taken);
     if ((rc = run_attn8(c, s, ll, ms, decode, qkv, nqkv, c->ws_attn.p, st))) return rc;
     {
         ProfScope ps(c, 0, st);
@@ -1439,14 +1484,20 @@ int run_attn_phase8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode,
     return mark_meta8_used(c, ms, st);
 }
 
+// The workspace of the MLP phase: the activation, gate and up in front of it where a product does not fuse SwiGLU, and the RMSNorm factors.
+int mlp_ws(ss_ctx* c, Shard* s, int ll, int T, size_t* act_bytes, size_t* gu_bytes) {
+    *act_bytes = align256((size_t)T * s->f_l * c->es);
+    *gu_bytes = s->w[ll].gu_interleaved ? 0 : align256((size_t)T * 2 * s->f_l * c->es);
+    return ensure_buf(c, c->ws_act, *act_bytes + *gu_bytes + (size_t)T * sizeof(float));
+}
+
 int run_mlp_phase(ss_ctx* c, Shard* s, int ll, int T, const void* x1, void* out, bool residual, hipStream_t st) {
     const ss_model_cfg& m = c->m;
     const LayerW& w = s->w[ll];
     const int H = m.hidden, F = s->f_l;
     int rc;
-    // the activation, gate and up in front of it where a product does not fuse SwiGLU, and the RMSNorm factors
-    const size_t act_bytes = align256((size_t)T * F * c->es), gu_bytes = w.gu_interleaved ? 0 : align256((size_t)T * 2 * F * c->es);
-    if ((rc = ensure_buf(c, c->ws_act, act_bytes + gu_bytes + (size_t)T * sizeof(float)))) return rc;
+    size_t act_bytes, gu_bytes;
+    if ((rc = mlp_ws(c, s, ll, T, &act_bytes, &gu_bytes))) return rc;
     void* gu = (uint8_t*)c->ws_act.p + act_bytes;
     float* rs = (float*)((uint8_t*)gu + gu_bytes);
     SplitWs ws;
@@ -1506,6 +1557,8 @@ int layer_call(ss_ctx* c, const ss_shard_desc* d, int layer, int phase, const ss
         return run_mlp_phase(c, s, ll, (int)T, x_in, out, residual, st);
     }
     if ((rc = ensure_buf(c, c->ws_x1, (size_t)T * c->m.hidden * c->es))) return rc;
+    size_t act, gu;                          // a cache in 8 bits does not take every batch twice: what can fail comes before its write
+    if (s->kv8 && T > 0 && T <= (1 << 30) && (rc = mlp_ws(c, s, ll, (int)T, &act, &gu))) return rc;
     if ((rc = attn_phase(c, s, ll, b, decode, x_in, c->ws_x1.p, true, st))) return rc;
     return run_mlp_phase(c, s, ll, (int)T, c->ws_x1.p, out, true, st);
 }
@@ -2831,9 +2884,11 @@ int kv8_call(ss_ctx* c, const ss_shard_desc* d, int layer, const ss_batch* b, co
     hipStream_t st = (hipStream_t)stream;
     if ((rc = refuse_capture(c, st))) return rc;
     if ((rc = ensure_pools(c, s))) return rc;
+    Taken8 taken;
     Meta8Slot* ms = nullptr;
     const int ll = layer - d->layer_begin;
-    if ((rc = prepare8(c, s, ll, b, what == 2, write, what != 0, &ms))) return rc;
+    if ((rc = prepare8(c, s, ll, b, what == 2, write, what != 0, &taken, &ms))) return rc;
+    if (what && (rc = attn8_ready(c, s, ms, what == 2))) return rc;
     if (ms->pending) {
         HIP_TRY(c, ssk::upload(ms->job.src, ms->job.dst, (size_t)ms->job.n16 * 16, st));
         ms->pending = false;
@@ -2841,6 +2896,7 @@ int kv8_call(ss_ctx* c, const ss_shard_desc* d, int layer, const ss_batch* b, co
     if (write) {
         ProfScope ps(c, 4, st);
         K_TRY(c, SSK_CALL(c, kv8_write, x->k, x->k_stride, x->v, x->v_stride, s->nkv_l, hd, ms->b, s->kv8_layers[ll], st));
+        kv8_written(s, ll, ms, &taken);
     }
     if (what && (rc = run_attn8(c, s, ll, ms, what == 2, x->q, x->q_stride, out, st))) return rc;
     return mark_meta8_used(c, ms, st);
