@@ -1116,12 +1116,19 @@ int meta8_slot(ss_ctx* c, size_t total, Meta8Slot** out) {
     return SS_OK;
 }
 
-int mark_meta8_used(ss_ctx* c, Meta8Slot* ms, hipStream_t stream) {
-    if (!ms->done) HIP_TRY(c, hipEventCreateWithFlags(&ms->done, hipEventDisableTiming));
-    HIP_TRY(c, hipEventRecord(ms->done, stream));
-    ms->in_flight = true;
-    return SS_OK;
-}
+// A slot in use by a call: whichever way the call ends, the slot's images are not written again before what it queued is through.
+struct Meta8Use {
+    Meta8Slot* ms;
+    hipStream_t st;
+    Meta8Use(Meta8Slot* ms_, hipStream_t st_) : ms(ms_), st(st_) {}
+    Meta8Use(const Meta8Use&) = delete;
+    ~Meta8Use() {
+        ms->in_flight = true;
+        if (hipEventRecord(ms->done, st) == hipSuccess) return;
+        (void)hipGetLastError();
+        (void)hipStreamSynchronize(st);
+    }
+};
 
 // Arrays of one image, each at a multiple of 64 bytes.
 struct Image {
@@ -1453,6 +1460,7 @@ int run_attn_phase8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode,
     Taken8 taken;
     Meta8Slot* ms = nullptr;
     if ((rc = prepare8(c, s, ll, b, decode, true, true, &taken, &ms)) || (rc = attn8_ready(c, s, ms, decode))) return rc;
+    const Meta8Use use(ms, st);
     const int T = ms->b.T, H = m.hidden, d = m.head_dim;
     const int nqkv = (s->nq_l + 2 * s->nkv_l) * d;
     const size_t qkv_bytes = align256((size_t)T * nqkv * c->es);
@@ -1481,7 +1489,7 @@ int run_attn_phase8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode,
         K_TRY(c, SSK_CALL(c, gemm_nt, c->ws_attn.p, s->nq_l * d, w.wo_t, out, H, residual ? x_in : nullptr, T, H,
                               s->nq_l * d, residual ? ssk::EPI_RESIDUAL : ssk::EPI_STORE, c->force_generic, st, ws.p, ws.bytes, c->gemm_rounds));
     }
-    return mark_meta8_used(c, ms, st);
+    return SS_OK;
 }
 
 // The workspace of the MLP phase: the activation, gate and up in front of it where a product does not fuse SwiGLU, and the RMSNorm factors.
@@ -2889,6 +2897,7 @@ int kv8_call(ss_ctx* c, const ss_shard_desc* d, int layer, const ss_batch* b, co
     const int ll = layer - d->layer_begin;
     if ((rc = prepare8(c, s, ll, b, what == 2, write, what != 0, &taken, &ms))) return rc;
     if (what && (rc = attn8_ready(c, s, ms, what == 2))) return rc;
+    const Meta8Use use(ms, st);
     if (ms->pending) {
         HIP_TRY(c, ssk::upload(ms->job.src, ms->job.dst, (size_t)ms->job.n16 * 16, st));
         ms->pending = false;
@@ -2899,7 +2908,7 @@ int kv8_call(ss_ctx* c, const ss_shard_desc* d, int layer, const ss_batch* b, co
         kv8_written(s, ll, ms, &taken);
     }
     if (what && (rc = run_attn8(c, s, ll, ms, what == 2, x->q, x->q_stride, out, st))) return rc;
-    return mark_meta8_used(c, ms, st);
+    return SS_OK;
 }
 
 }  // namespace
@@ -3004,6 +3013,7 @@ static int kv8_evict_call(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_
     if ((rc = meta8_slot(c, im.total, &ms))) return rc;
     im.write(ms->host);
     ms->pending = false;
+    const Meta8Use use(ms, st);
     HIP_TRY(c, ssk::upload(ms->job.src, ms->job.dst, (size_t)ms->job.n16 * 16, st));
     ssk::Kv8Evict e{};
     e.page_tables = (const int32_t*)(ms->dev + o_pt);
@@ -3028,7 +3038,7 @@ static int kv8_evict_call(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_
         }
     }
     s->version++;
-    return mark_meta8_used(c, ms, st);
+    return SS_OK;
 }
 
 int ss_kv8_weights(ss_ctx* c, const ss_shard_desc* d, int dir, const int64_t* seq_ids, int n, float* buf, void* stream) {
