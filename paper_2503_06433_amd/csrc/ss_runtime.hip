@@ -2613,20 +2613,20 @@ int ss_weights_read(ss_ctx* c, const ss_shard_desc* d, int layer, int which, voi
 
 int ss_layer_prefill(ss_ctx* c, const ss_shard_desc* d, int layer, int phase, const ss_batch* b, const void* x_in,
                      void* out, void* stream) {
-    return layer_call(c, d, layer, phase, b, x_in, out, stream, false);
+    return guarded(c, [&] { return layer_call(c, d, layer, phase, b, x_in, out, stream, false); });
 }
 
 int ss_layer_decode(ss_ctx* c, const ss_shard_desc* d, int layer, int phase, const ss_batch* b, const void* x_in,
                     void* out, void* stream) {
-    return layer_call(c, d, layer, phase, b, x_in, out, stream, true);
+    return guarded(c, [&] { return layer_call(c, d, layer, phase, b, x_in, out, stream, true); });
 }
 
 int ss_layers_prefill(ss_ctx* c, const ss_shard_desc* d, const ss_batch* b, const void* x_in, void* out, void* stream) {
-    return layers_call(c, d, b, x_in, out, stream, false);
+    return guarded(c, [&] { return layers_call(c, d, b, x_in, out, stream, false); });
 }
 
 int ss_layers_decode(ss_ctx* c, const ss_shard_desc* d, const ss_batch* b, const void* x_in, void* out, void* stream) {
-    return layers_call(c, d, b, x_in, out, stream, true);
+    return guarded(c, [&] { return layers_call(c, d, b, x_in, out, stream, true); });
 }
 
 // `out_id`: swap-out that a swap-in of the same list follows (written), swap-in that follows it (read), or null.
