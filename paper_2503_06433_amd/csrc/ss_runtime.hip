@@ -1274,7 +1274,8 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
     std::vector<int32_t> before(n), end(n), slot(n), pos(n);
     int64_t T = 0, seen = 0;
     int max_q = 0, max_seen = 0;
-    size_t more = 0, fresh = 0;
+    size_t more = 0;
+    std::vector<int64_t> unknown;                           // sequences that the shard has none of
     ++c->batches;
     for (int i = 0; i < n; ++i) {
         const int64_t id = b->seq_ids[i];
@@ -1309,23 +1310,22 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
         pos[i] = at;
         const size_t need = (size_t)(end[i] + ps - 1) / ps, pages = st ? st->pages.size() : 0;
         if (need > pages) more += need - pages;
-        fresh += !st;
+        if (!st) unknown.push_back(id);
         T += ql;
         seen += (cached + ql + ps - 1) / ps;
         max_q = std::max(max_q, ql);
         max_seen = std::max(max_seen, cached + ql);
     }
-    for (int i = 0; fresh > 1 && i < n; ++i)                // sequences that nobody knows yet are compared among themselves
-        if (!s->seqs.count(b->seq_ids[i]))
-            for (int j = 0; j < i; ++j)
-                if (b->seq_ids[j] == b->seq_ids[i]) return fail(c, SS_EINVAL, "sequence %lld is listed twice", (long long)b->seq_ids[i]);
+    std::sort(unknown.begin(), unknown.end());
+    const auto twice = std::adjacent_find(unknown.begin(), unknown.end());
+    if (twice != unknown.end()) return fail(c, SS_EINVAL, "sequence %lld is listed twice", (long long)*twice);
     if (T > (1 << 30) || (attend && (int64_t)max_q * (s->nq_l / s->nkv_l) > (1 << 30))) return fail(c, SS_EINVAL, "batch too large");
     if (attend && (n > 65535 || s->nq_l > 65535)) return fail(c, SS_EINVAL, "batch too large: %d sequences, %d query heads", n, s->nq_l);
     if (decode && s->kv8_weights && seen > INT32_MAX) return fail(c, SS_EINVAL, "batch too large: it sees %lld pages", (long long)seen);
     if (more > s->free_pages.size())
         return fail(c, SS_ENOMEM, "page pool exhausted: the batch needs %zu more pages, %zu free", more, s->free_pages.size());
-    if (fresh > s->free_slots.size())
-        return fail(c, SS_ENOMEM, "%zu new sequences, %zu of %d left in the cache in 8 bits", fresh, s->free_slots.size(), s->kv8_slots);
+    if (unknown.size() > s->free_slots.size())
+        return fail(c, SS_ENOMEM, "%zu new sequences, %zu of %d left in the cache in 8 bits", unknown.size(), s->free_slots.size(), s->kv8_slots);
     // a swap-out that has not run yet reads the open blocks, a swap-in the tokens wait for
     wait_seqs_idle(c, s, b->seq_ids, n);
     if (write) {
