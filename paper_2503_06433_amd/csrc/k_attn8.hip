@@ -156,6 +156,15 @@ constexpr float TOP_EXP = 14.f;
 #else
 constexpr float TOP_EXP = 0.f;
 #endif
+// The power of two that an open block's V is divided by, for a largest magnitude of `big`: it then lies below 128, as a full block's whole
+// numbers do.  Half has no room for that from 128 on: what is some 2^-16 of the largest would fall below the type's normal range and be
+// rounded (0.001 next to 60000 came out as 0.001007).  It is left as it is there; the block's weights are then up to 2^9 further
+// below the largest one than they would be.
+__device__ __forceinline__ int open_exponent(float big) {
+    int e = big > 0.f ? (int)(__float_as_uint(big) >> 23) - 127 - 6 : (int)LV_ZERO;
+    if (TOP_EXP > 0.f && e > 0) e = 0;
+    return e < (int)LV_MIN ? (int)LV_MIN : e;
+}
 constexpr float ONE_127 = 1.f / 127.f;               // a step is formed with it: one more rounding of 2^-24, ten operations less than the quotient
 __device__ __forceinline__ void v_step(float amax, float& lv, float& inv) {
     const float l = __builtin_amdgcn_logf(amax * ONE_127);
@@ -311,7 +320,7 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
     }
     if (open_here) {
         // Tokens 4 g4 + v of the open block, in the model's type, in the first four of the group's eight slots of the second product.  V is
-        // scaled by a power of two (exact) to below 128, as the whole numbers of a full block are.
+        // scaled by a power of two (open_exponent).
         const int cnt = p - full * 16 + 1;
         const bf16_t* ko = (const bf16_t*)kv.open + ((size_t)slot * 2 * n_kv + g) * 16 * D;
         const bf16_t* vo = ko + (size_t)n_kv * 16 * D;
@@ -336,9 +345,7 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
             for (int v = 0; v < 4; ++v)
                 if (4 * g4 + v < cnt) big = fmaxf(big, fabsf(bf2f(raw[t][v])));
         big = wave_max(big);
-        int e = big > 0.f && big < INFINITY ? (int)(__float_as_uint(big) >> 23) - 127 - 6 : big > 0.f ? 0 : (int)LV_ZERO;
-        e = e < (int)LV_MIN ? (int)LV_MIN : e;
-        const float lv = (float)e;
+        const float lv = big < INFINITY ? (float)open_exponent(big) : 0.f;
         float top = -INFINITY;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
@@ -623,9 +630,8 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
     f32x16_t o[DT];
     float r, l;
 
-    // The open block's page of the tile that is multiplied next, over what `store` brought there: the model's type as it is, V times a
-    // power of two that brings it below 128 and without values that are not finite; tokens that have such are marked, their
-    // weight is to be NaN.
+    // The open block's page of the tile that is multiplied next, over what `store` brought there: the model's type as it is, V divided by
+    // a power of two (open_exponent) and without values that are not finite; tokens that have such are marked, their weight is to be NaN.
     auto store_open = [&](uint32_t st, Steps& s) {
         const bf16_t* ko = (const bf16_t*)kv.open + ((size_t)b.slot[sq] * 2 * n_kv + g) * 16 * D;
         const bf16_t* vo = ko + (size_t)n_kv * 16 * D;
@@ -650,8 +656,7 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
 #pragma unroll
         for (int i = 32; i > 0; i >>= 1) mark |= __shfl_xor(mark, i, 64);
         bad = mark;
-        int e = big > 0.f ? (int)(__float_as_uint(big) >> 23) - 127 - 6 : (int)LV_ZERO;
-        e = e < (int)LV_MIN ? (int)LV_MIN : e;
+        const int e = open_exponent(big);
         if (my_page == (full & 3)) s = Steps{scale_log2e, (float)e, exp2_fast((float)-e)};
         if ((full & 3) != pg_w) return;
         if (does_k) {
