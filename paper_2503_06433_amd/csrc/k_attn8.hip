@@ -146,9 +146,11 @@ __device__ __forceinline__ Frag8 widen8(uint32_t a, uint32_t b) {
 
 // The weights of a block are kept times its V step: the second product then takes V's whole numbers as they are, and a 16-bit
 // weight is rounded relative to what it contributes.  lv: log 2 of the step; inv brings the sum of such weights back.  A block of
-// zeros adds to the sum alone: any step serves, this one lies below those of half values and far above underflow.  Steps below
-// 2^-100 count as that.
-constexpr float LV_ZERO = -40.f, LV_MIN = -100.f;
+// zeros adds to the sum alone: any step serves, this one lies below those of half values and far above underflow.
+// The reference r of the exponents follows the largest score + lv, but with an lv of at least LV_REF: the sum, of exp2(score - r), of a cache
+// that holds tiny values only would pass the largest float otherwise.  Steps below 2^LV_MIN, of values below 127 * 2^-126, count as that
+// (the next smaller ones are no normal floats).
+constexpr float LV_ZERO = -40.f, LV_REF = -100.f, LV_MIN = -126.f;
 // Half: the largest weight is 2^14 instead of 1, so that those of 2^-28 of it are still in the type's normal range.  With 1 a token
 // of weight 2^-16 is rounded to 2^-9 of itself, which shows in outputs whose heavy tokens happen to have a value of 0.
 #ifdef SS_HALF_F16
@@ -156,6 +158,7 @@ constexpr float TOP_EXP = 14.f;
 #else
 constexpr float TOP_EXP = 0.f;
 #endif
+__device__ __forceinline__ float lv_ref(float lv) { return TOP_EXP > 0.f ? lv : fmaxf(lv, LV_REF); }  // half has no steps below 2^-31
 // The power of two that an open block's V is divided by, for a largest magnitude of `big`: it then lies below 128, as a full block's whole
 // numbers do.  Half has no room for that from 128 on: what is some 2^-16 of the largest would fall below the type's normal range and be
 // rounded (0.001 next to 60000 came out as 0.001007).  It is left as it is there; the block's weights are then up to 2^9 further
@@ -163,7 +166,7 @@ constexpr float TOP_EXP = 0.f;
 __device__ __forceinline__ int open_exponent(float big) {
     int e = big > 0.f ? (int)(__float_as_uint(big) >> 23) - 127 - 6 : (int)LV_ZERO;
     if (TOP_EXP > 0.f && e > 0) e = 0;
-    return e < (int)LV_MIN ? (int)LV_MIN : e;
+    return e < (int)LV_REF ? (int)LV_REF : e;
 }
 constexpr float ONE_127 = 1.f / 127.f;               // a step is formed with it: one more rounding of 2^-24, ten operations less than the quotient
 __device__ __forceinline__ void v_step(float amax, float& lv, float& inv) {
@@ -277,7 +280,7 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
 #pragma unroll
                 for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4_t*>(sp + (size_t)pg * n_q * 16 + 4 * i) = s[i];
             }
-            top = over_groups(top + lv) - TOP_EXP;
+            top = over_groups(top + lv_ref(lv)) - TOP_EXP;
             if (__any(top > r)) rescale(fmaxf(top, r));
             const float off = lv - r;
             float rs = 0.f;
@@ -693,7 +696,7 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
         float m = max3(s[0], s[1], s[2]);
 #pragma unroll
         for (int v = 3; v < 15; v += 2) m = max3(m, s[v], s[v + 1]);
-        const float top = max_of_halves(fmaf(fmaxf(m, s[15]), ks, lv)) - TOP_ROW;
+        const float top = max_of_halves(fmaf(fmaxf(m, s[15]), ks, lv_ref(lv))) - TOP_ROW;
         const bool moved = top - r > LAG;                            // also in the first step (r = -infinity)
         const float alpha = moved ? exp2_fast(r - top) : 1.f;
         r = moved ? top : r;

@@ -68,3 +68,14 @@ def test_small_values_next_to_large_ones_in_an_open_block_of_halves(big, d):
         qv[:, :, 0] = 32
         q, k, v = ((x, _dev(r, wl.F16)) for x, r in (wl.quantize(a, wl.F16) for a in (qv, kv_, vv)))
         _both(c, q, k, v)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("scale", [-118, -112, -100, -60, 60, 100, 120])
+def test_caches_of_small_and_of_large_values(scale, d):
+    """All values of a cache around 2^scale."""
+    rng = np.random.default_rng(42)
+    c = Cache(wl.BF16, 6, 2, d, pages=300, weights=True)
+    for n in (5, 47, 1100):
+        v, r = wl.quantize(np.clip(rng.normal(size=(n, 2, d)), -3, 3) * 2.0 ** scale, wl.BF16)
+        _both(c, c.tokens(rng, n, 6), c.tokens(rng, n, 2), (v, _dev(r, wl.BF16)))
