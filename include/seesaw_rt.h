@@ -259,7 +259,8 @@ int ss_kv_import_dev(ss_ctx*, const ss_shard_desc*, const int64_t* seq_ids, cons
  *   qkv->q over what the cache holds: the query at position p sees positions 0 .. p, query head a the kv head
  *   a / (n_q / n_kv) of the shard's, scores are divided by sqrt(head_dim).  With k and v both NULL nothing is
  *   written: the tokens have to be there.
- *   16-bit models: steps A / 127 of V below 2^-126 (values below 1.5e-36) count as that.
+ *   16-bit models: steps A / 127 of V below 2^-126 (values below 1.5e-36) count as that. What is 2^-100 of
+ *   the largest values that a query sees, and less, may be missing from its output.
  *   (A query that sees a value that is not finite in the open block has at least that element not finite, and may have
  *   NaN in the head's others; one that does not see it is not touched.)
  * ss_kv8_attn_decode: the same, one token per sequence, which adds the softmax weights of all query heads of a kv

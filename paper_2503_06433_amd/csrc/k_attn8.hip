@@ -168,6 +168,16 @@ __device__ __forceinline__ int open_exponent(float big) {
     if (TOP_EXP > 0.f && e > 0) e = 0;
     return e < (int)LV_REF ? (int)LV_REF : e;
 }
+// Brain floats: the steps of a head's blocks can lie so far apart that a weight (times its step) underflows although its token has its part in
+// the sum: blocks of zeros or of small values beside values 2^90 times as large.  Where a block's largest weight is below 2^FAR its
+// sum is formed with exponents of its own, from 0 down.  References that move that far are followed in two steps of half the
+// distance, which the sum survives.  Half's steps, 2^-40 to 2^9, are never that far apart, nor are those from 2^-NEAR to 2^NEAR (a token
+// that has 2^-30 of the largest score's weight is at 2^-120 there).
+constexpr bool WIDE = TOP_EXP == 0.f;
+constexpr float FAR = -100.f, NEAR = 45.f;
+__device__ __forceinline__ float half_way(float d) { return exp2_fast(WIDE ? 0.5f * d : d); }
+__device__ __forceinline__ float twice(float x, float a) { return WIDE ? x * a * a : x * a; }
+__device__ __forceinline__ bool far_below(float top) { return WIDE && top < FAR && top > -INFINITY; }
 constexpr float ONE_127 = 1.f / 127.f;               // a step is formed with it: one more rounding of 2^-24, ten operations less than the quotient
 __device__ __forceinline__ void v_step(float amax, float& lv, float& inv) {
     const float l = __builtin_amdgcn_logf(amax * ONE_127);
@@ -216,9 +226,10 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
     float* sp = WEIGHTS ? scores + ((size_t)b.pg_off[sq] * n_q + a) * 16 : nullptr;      // [page][n_q][16]
 
     auto rescale = [&](float top) {
-        const float alpha = exp2_fast(r - top);
+        const float a = r < top ? half_way(r - top) : 1.f;
+        const float alpha = twice(1.f, a);
         r = top;
-        l *= alpha;
+        l = twice(l, a);
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -280,10 +291,18 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
 #pragma unroll
                 for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4_t*>(sp + (size_t)pg * n_q * 16 + 4 * i) = s[i];
             }
+            const float own = top;
             top = over_groups(top + lv_ref(lv)) - TOP_EXP;
             if (__any(top > r)) rescale(fmaxf(top, r));
             const float off = lv - r;
-            float rs = 0.f;
+            float rs = 0.f, apart = 0.f;
+            if (__builtin_expect(__any(far_below(own + off)), 0)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) apart += exp2_fast(s[i][v] - own);
+                apart = twice(apart, half_way(own - r));
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -292,7 +311,7 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
                     s[i][v] = whole || 4 * i + v <= seen ? w : 0.f;      // the step of a hidden block may not be a number
                     rs += s[i][v];
                 }
-            l += whole || seen >= 0 ? rs * inv : 0.f;
+            l += whole || seen >= 0 ? far_below(own + off) ? apart : rs * inv : 0.f;
             Frag8 pa, pb;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -357,13 +376,15 @@ __global__ __launch_bounds__(64) void attn8_decode_kernel(const bf16_t* __restri
         }
         if (WEIGHTS && mine) *reinterpret_cast<f32x4_t*>(sp + (size_t)full * n_q * 16 + 4 * g4) = s;
         rescale(fmaxf(r, over_groups(top + lv) - TOP_EXP));
-        float rs = 0.f;
+        const float off = lv - r;
+        float rs = 0.f, apart = 0.f;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            s[v] = 4 * g4 + v < cnt ? exp2_fast(s[v] + (lv - r)) : 0.f;
+            apart += 4 * g4 + v < cnt ? exp2_fast(s[v] - top) : 0.f;
+            s[v] = 4 * g4 + v < cnt ? exp2_fast(s[v] + off) : 0.f;
             rs += s[v];
         }
-        l += rs * exp2_fast(-lv);
+        l += far_below(top + off) ? twice(apart, half_way(top - r)) : rs * exp2_fast(-lv);
         Frag8 pf;
         pf.w[0] = pack_bf16x2(s[0], s[1]);
         pf.w[1] = pack_bf16x2(s[2], s[3]);
@@ -426,15 +447,15 @@ __global__ __launch_bounds__(256) void attn8_merge_kernel(const float* __restric
             mx = fmaxf(mx, m[u]);
         }
         const float ref = mx == -INFINITY ? 0.f : mx;
-        const float alpha = exp2_fast(M - ref);
+        const float a = half_way(M - ref);
         M = mx;
-        num *= alpha;
-        den *= alpha;
+        num *= twice(1.f, a);
+        den = twice(den, a);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const float w = exp2_fast(m[u] - ref);
-            num += w * v[u];
-            den += w * l[u];
+            const float w = half_way(m[u] - ref);
+            num += twice(1.f, w) * v[u];
+            den += twice(l[u], w);
         }
     }
     if constexpr (SPLIT > 1) {
@@ -445,15 +466,15 @@ __global__ __launch_bounds__(256) void attn8_merge_kernel(const float* __restric
         float mx = M;
 #pragma unroll
         for (int u = 1; u < SPLIT; ++u) mx = fmaxf(mx, part[u][D]);
-        const float ref = mx == -INFINITY ? 0.f : mx, w0 = exp2_fast(M - ref);
+        const float ref = mx == -INFINITY ? 0.f : mx, w0 = half_way(M - ref);
         M = mx;
-        num *= w0;
-        den *= w0;
+        num *= twice(1.f, w0);
+        den = twice(den, w0);
 #pragma unroll
         for (int u = 1; u < SPLIT; ++u) {
-            const float w = exp2_fast(part[u][D] - ref);
-            num += w * *reinterpret_cast<const f32x4_t*>(&part[u][e]);
-            den += w * part[u][D + 1];
+            const float w = half_way(part[u][D] - ref);
+            num += twice(1.f, w) * *reinterpret_cast<const f32x4_t*>(&part[u][e]);
+            den += twice(part[u][D + 1], w);
         }
     }
     vec16 w;
@@ -574,7 +595,7 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
         if (does_v) w.v = *reinterpret_cast<const vec16*>(kv.v + page + at);
         w.amax = *reinterpret_cast<const float2*>(kv.amax + ((size_t)ids.page * n_kv + ids.g) * 2);
     };
-    struct Steps { float ks, lv, inv; };                                 // of the lane's page
+    struct Steps { float ks, lv, inv; bool wide; };                      // of the lane's page; whether one of the tile's is not NEAR
     uint32_t stage = 0;                                                  // of the tile that is multiplied; the next one is in the other
     // LDS image of the next tile; returns the steps of its pages
     auto store = [&](uint32_t st, const Raw& w) {
@@ -582,6 +603,7 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
         s.ks = w.amax.x * (ONE_127 * scale_log2e);
         s.ks = s.ks < 1e-37f ? 1e-37f : s.ks;                            // a block of zeros: any step, but no infinity times zero
         v_step(w.amax.y, s.lv, s.inv);
+        s.wide = WIDE && __any(fabsf(s.lv) > NEAR);
         if (does_k) {
             *lds(st + k_write) = widen8(w.k.w[0], w.k.w[1]).q;
             *lds((st + k_write) ^ 16) = widen8(w.k.w[2], w.k.w[3]).q;
@@ -660,7 +682,7 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
         for (int i = 32; i > 0; i >>= 1) mark |= __shfl_xor(mark, i, 64);
         bad = mark;
         const int e = open_exponent(big);
-        if (my_page == (full & 3)) s = Steps{scale_log2e, (float)e, exp2_fast((float)-e)};
+        if (my_page == (full & 3)) s = Steps{scale_log2e, (float)e, exp2_fast((float)-e), s.wide};
         if ((full & 3) != pg_w) return;
         if (does_k) {
             const vec16* kr = reinterpret_cast<const vec16*>(ko + k_tok * D + k_piece * 16);
@@ -686,7 +708,8 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
         }
     };
 
-    // 32 tokens of scores, of the lane's page 16, become weights.  `hidden`: some of them are not to be seen by every row.
+    // 32 tokens of scores, of the lane's page 16, become weights.  `hidden`: some of them are not to be seen by every row, or the steps that
+    // the row has met need not be NEAR each other.
     auto softmax = [&](auto hidden_c, f32x16_t& s, float ks, float lv, float inv, int t0, Frag8& pA, Frag8& pB) {
         constexpr bool hidden = decltype(hidden_c)::value;
         if constexpr (hidden) {
@@ -696,12 +719,23 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
         float m = max3(s[0], s[1], s[2]);
 #pragma unroll
         for (int v = 3; v < 15; v += 2) m = max3(m, s[v], s[v + 1]);
-        const float top = max_of_halves(fmaf(fmaxf(m, s[15]), ks, lv_ref(lv))) - TOP_ROW;
+        m = fmaxf(m, s[15]);
+        const float top = max_of_halves(fmaf(m, ks, hidden ? lv_ref(lv) : lv)) - TOP_ROW;
         const bool moved = top - r > LAG;                            // also in the first step (r = -infinity)
-        const float alpha = moved ? exp2_fast(r - top) : 1.f;
+        const float a = !moved ? 1.f : hidden ? half_way(r - top) : exp2_fast(r - top), alpha = hidden ? twice(1.f, a) : a;
         r = moved ? top : r;
         const float off = lv - r;
-        float sum = 0.f;
+        float sum = 0.f, apart = 0.f;
+        bool far = false;
+        if constexpr (hidden && WIDE) {
+            const float own = fmaf(m, ks, off);                      // exponent of the largest weight
+            far = far_below(own);
+            if (__builtin_expect(__any(far), 0)) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) apart += exp2_fast((s[v] - m) * ks);
+                apart = twice(apart, half_way(fmaf(m, ks, -r)));
+            }
+        }
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             s[v] = exp2_fast(fmaf(s[v], ks, off));
@@ -711,8 +745,8 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
             }
             sum += s[v];
         }
-        sum *= inv;
-        l = l * alpha + (hidden && t0 > p ? 0.f : sum);
+        sum = far ? apart : sum * inv;
+        l = (hidden ? twice(l, a) : l * a) + (hidden && t0 > p ? 0.f : sum);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             pA.w[i] = pack_bf16x2(s[2 * i], s[2 * i + 1]);
@@ -807,9 +841,9 @@ __global__ __launch_bounds__(512) void attn8_prefill_kernel(const bf16_t* __rest
             stage ^= STAGE;
             publish();
         };
-        // first the tiles that every row of the wave sees all of
+        // first the tiles that every row of the wave sees all of, while all steps are NEAR
         int it = tile0;
-        for (; it < n_tiles && active && it * 64 + 63 <= wave_first; ++it) {
+        for (; it < n_tiles && active && it * 64 + 63 <= wave_first && !cur.wide; ++it) {
             bring();
             tile(std::false_type{}, it, cur);
             next();
@@ -885,15 +919,15 @@ __global__ __launch_bounds__(256) void attn8_join_kernel(const float* __restrict
             }
             mx = fmaxf(mx, m[u]);
         }
-        const float ref = mx == -INFINITY ? 0.f : mx, alpha = exp2_fast(M - ref);
+        const float ref = mx == -INFINITY ? 0.f : mx, a = half_way(M - ref);
         M = mx;
-        num *= alpha;
-        den *= alpha;
+        num *= twice(1.f, a);
+        den = twice(den, a);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const float w = exp2_fast(m[u] - ref);
-            num += w * v[u];
-            den += w * l[u];
+            const float w = half_way(m[u] - ref);
+            num += twice(1.f, w) * v[u];
+            den += twice(l[u], w);
         }
     }
     *reinterpret_cast<uint2*>(out + ((int64_t)(rec[3] + row / G) * n_q + rec[1] * G + row % G) * D + e) =

@@ -79,3 +79,25 @@ def test_caches_of_small_and_of_large_values(scale, d):
     for n in (5, 47, 1100):
         v, r = wl.quantize(np.clip(rng.normal(size=(n, 2, d)), -3, 3) * 2.0 ** scale, wl.BF16)
         _both(c, c.tokens(rng, n, 6), c.tokens(rng, n, 2), (v, _dev(r, wl.BF16)))
+
+
+# powers of two of a cycle of blocks; None: zeros
+CYCLES = [(None, 110), (110, None), (None, None, None, None, None, 115, None), (0, 110), (110, 0, -60), (-100, None, 0, 100, -30),
+          (-110, 0), (0, -110, -110, -110, -110), (None, -110),
+          (0,) * 40 + (110,) + (None,) * 20 + (0,) * 30]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cycle", CYCLES, ids=["_".join("zero" if x is None else str(x) for x in c[:8]) for c in CYCLES])
+def test_blocks_of_very_different_size_side_by_side(cycle, d):
+    """Weights of similar size on blocks of zeros, of ordinary, tiny and huge values: what a block does not add to the output it still adds
+    to the sum of weights."""
+    rng = np.random.default_rng(43)
+    c = Cache(wl.BF16, 3, 1, d, pages=500, weights=True)
+    for n in (13, 16 * len(cycle) + 7, 700, 2500):
+        x = np.clip(rng.normal(size=(n, 1, d)), -3, 3)
+        for b in range(0, n, 16):
+            e = cycle[b // 16 % len(cycle)]
+            x[b:b + 16] *= 0.0 if e is None else 2.0 ** e
+        v, r = wl.quantize(x, wl.BF16)
+        _both(c, c.tokens(rng, n, 3, 0.5), c.tokens(rng, n, 1, 0.5), (v, _dev(r, wl.BF16)))
