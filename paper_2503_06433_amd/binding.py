@@ -291,6 +291,8 @@ class Context:
     # ---- layers
     def _batch(self, seq_ids, q_lens, kv_before):
         s, q, b = _i64(seq_ids), _i32(q_lens), _i32(kv_before)
+        if len(q) < len(s) or len(b) < len(s):
+            raise ValueError("%d sequences, %d lengths, %d positions" % (len(s), len(q), len(b)))
         bt = _Batch(len(s), _p(s), _p(q), _p(b))
         return bt, (s, q, b)
 
@@ -342,6 +344,8 @@ class Context:
 
     def kv_import_dev(self, desc, seq_ids, lens, staging, stream=0):
         s, l = _i64(seq_ids), _i32(lens)
+        if len(l) < len(s):
+            raise ValueError("%d sequences, %d lengths" % (len(s), len(l)))
         self._ck(self.lib.ss_kv_import_dev(self.h, C.byref(desc), _p(s),
                                            _p(l), len(s), _ptr(staging), stream))
 
