@@ -270,6 +270,7 @@ int ss_kv_import_dev(ss_ctx*, const ss_shard_desc*, const int64_t* seq_ids, cons
  *   back to back, so that they may be parts of one fused row.  out must not overlap them.
  * ss_kv8_weights: the accumulated weights of whole sequences out of (SS_OUT) or into (SS_IN) buf, device,
  *   [seq][layer_local][head_local][token], sequences back to back.  Newly written or imported tokens have weight 0.
+ * ss_kv8_weights_len: how many weights that is.
  * ss_kv8_evict: cuts every listed sequence of more than keep[i] tokens to keep[i] (>= 1), in every layer and kv head on its own: the
  *   `recent` newest tokens stay (all keep[i] if recent is larger), of the others those of greatest weight, the
  *   earlier of equal ones; NaN counts as greatest.  They keep their order and weights and are put into blocks anew
@@ -288,6 +289,7 @@ int ss_kv8_write(ss_ctx*, const ss_shard_desc*, int layer, const ss_batch*, cons
 int ss_kv8_attn_prefill(ss_ctx*, const ss_shard_desc*, int layer, const ss_batch*, const ss_qkv*, void* out, void* stream);
 int ss_kv8_attn_decode(ss_ctx*, const ss_shard_desc*, int layer, const ss_batch*, const ss_qkv*, void* out, void* stream);
 int ss_kv8_weights(ss_ctx*, const ss_shard_desc*, int dir, const int64_t* seq_ids, int n, float* buf, void* stream);
+int ss_kv8_weights_len(ss_ctx*, const ss_shard_desc*, const int64_t* seq_ids, int n, int64_t* len_out);
 int ss_kv8_evict(ss_ctx*, const ss_shard_desc*, const int64_t* seq_ids, const int32_t* keep, int n, int recent, void* stream);
 
 /* ---- inspection (tests) ------------------------------------------------ */

@@ -118,6 +118,7 @@ def load_library():
         "ss_kv8_attn_prefill": (I, [V, D, I, P(_Batch), P(_Qkv), V, V]),
         "ss_kv8_attn_decode": (I, [V, D, I, P(_Batch), P(_Qkv), V, V]),
         "ss_kv8_weights": (I, [V, D, I, P(L), I, V, V]),
+        "ss_kv8_weights_len": (I, [V, D, P(L), I, P(L)]),
         "ss_kv8_evict": (I, [V, D, P(L), P(C.c_int32), I, I, V]),
         "ss_kv_page_table": (I, [V, D, L, P(C.c_int32), P(C.c_int32)]),
         "ss_kv_seq_len": (I, [V, D, L, P(C.c_int32)]),
@@ -147,7 +148,7 @@ def load_library():
 EXPORTED = ("ss_create ss_destroy ss_last_error ss_load_layer ss_host_weights_put ss_reshard_weights ss_weights_wait "
             "ss_weights_shard_bytes ss_weights_read ss_layer_prefill ss_layer_decode ss_layers_prefill ss_layers_decode ss_kv_swap "
             "ss_kv_reshard ss_sync ss_kv_jobs_issued ss_kv_wait ss_kv_free ss_host_tier_release ss_kv_export_dev ss_kv_import_dev "
-            "ss_kv8_enable ss_kv8_write ss_kv8_attn_prefill ss_kv8_attn_decode ss_kv8_weights ss_kv8_evict "
+            "ss_kv8_enable ss_kv8_write ss_kv8_attn_prefill ss_kv8_attn_decode ss_kv8_weights ss_kv8_weights_len ss_kv8_evict "
             "ss_kv_page_table ss_kv_seq_len ss_kv_read ss_host_tier_read ss_host_tier_used_bytes "
             "ss_kv_free_pages ss_load_head ss_embed ss_lm_head ss_lm_head_noalloc ss_get_config ss_offline_run ss_prof_enable ss_prof_read ss_prof_reset").split()
 
@@ -391,9 +392,16 @@ class Context:
         self._ck(self.lib.ss_kv8_attn_decode(self.h, C.byref(desc), layer, C.byref(bt), C.byref(qkv), self._attn_out(desc, q, out), stream))
 
     def kv8_weights(self, desc, direction, seq_ids, buf, stream=0):
-        """buf: float32 on the device, [sequence][layer][head][token] back to back."""
+        """buf: float32 tensor on the device, [sequence][layer][head][token] back to back."""
         s = _i64(seq_ids)
-        self._ck(self.lib.ss_kv8_weights(self.h, C.byref(desc), direction, _p(s), len(s), _ptr(buf), stream))
+        p, n = _p(s), C.c_int64(0)
+        self._ck(self.lib.ss_kv8_weights_len(self.h, C.byref(desc), p, len(s), C.byref(n)))
+        if not hasattr(buf, "data_ptr"):
+            raise ValueError("a tensor on the context's device expected")
+        if str(buf.dtype) != "torch.float32" or buf.device.index != self.runtime.device or buf.numel() < n.value or not buf.is_contiguous():
+            raise ValueError("%d contiguous elements of torch.float32 on the context's device expected, not %s of %s on %s" %
+                             (n.value, tuple(buf.shape), buf.dtype, buf.device))
+        self._ck(self.lib.ss_kv8_weights(self.h, C.byref(desc), direction, p, len(s), buf.data_ptr(), stream))
 
     def kv8_evict(self, desc, seq_ids, keep, recent, stream=0):
         s, k = _i64(seq_ids), _i32(keep)

@@ -3041,6 +3041,25 @@ static int kv8_evict_call(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_
     return SS_OK;
 }
 
+int ss_kv8_weights_len(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, int n, int64_t* len_out) {
+    return guarded(c, [&]() -> int {
+        if (!c) return SS_EINVAL;
+        if (!len_out || n < 0 || (n > 0 && !seq_ids)) return fail(c, SS_EINVAL, "bad arguments");
+        Shard* s = nullptr;
+        int rc = kv8_shard(c, d, &s);
+        if (rc) return rc;
+        if (!s->kv8_weights) return fail(c, SS_EINVAL, "the shard keeps no attention weights");
+        int64_t tokens = 0;
+        for (int i = 0; i < n; ++i) {
+            auto it = s->seqs.find(seq_ids[i]);
+            if (it == s->seqs.end()) return fail(c, SS_ENOENT, "sequence %lld not resident", (long long)seq_ids[i]);
+            tokens += it->second.len;
+        }
+        *len_out = tokens * s->n_layers_l * s->nkv_l;
+        return SS_OK;
+    });
+}
+
 int ss_kv8_weights(ss_ctx* c, const ss_shard_desc* d, int dir, const int64_t* seq_ids, int n, float* buf, void* stream) {
     return guarded(c, [&] { return kv8_weights_call(c, d, dir, seq_ids, n, buf, stream); });
 }
