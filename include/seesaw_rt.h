@@ -302,6 +302,8 @@ int ss_kv_read(ss_ctx*, const ss_shard_desc*, int64_t seq, int layer, void* host
 int ss_host_tier_read(ss_ctx*, int64_t seq, int layer, void* host_out);
 int64_t ss_host_tier_used_bytes(ss_ctx*);
 int64_t ss_kv_free_pages(ss_ctx*, const ss_shard_desc*);
+/* sequences that a shard in 8 bits still has room for; SS_EINVAL for other shards. */
+int64_t ss_kv8_free_seqs(ss_ctx*, const ss_shard_desc*);
 
 /* ---- helpers for the tiny whole-model configuration --------------------- */
 /* embed [vocab, H], gf [H], wlm [H, vocab]; host pointers, model dtype. */
@@ -338,7 +340,7 @@ int ss_get_config(ss_ctx*, ss_model_cfg* model_out, ss_runtime_cfg* rt_out);
  * of actions is unique):
  *   prefill stage: requests in arrival order; a batch takes requests while
  *     the prompt tokens stay within max_prefill_tokens (a longer prompt alone)
- *     and the prompts' pages fit gpu_kv_pages;
+ *     and the prompts' pages fit gpu_kv_pages (their number, for a shard in 8 bits, its max_seqs);
  *     every batch's cache is swapped out behind it; the stage ends when the
  *     next prompt does not fit in the store (host_tier_bytes / bytes per token
  *     over all layers) or nothing is left to prefill.  A request that wants one
@@ -346,8 +348,8 @@ int ss_get_config(ss_ctx*, ss_model_cfg* model_out, ss_runtime_cfg* rt_out);
  *   decode stage, per iteration: caches requested in the previous iteration
  *     come on board; while the head of the store fits (pages of its final
  *     length, prompt + outputs - 1 tokens, next to those promised to admitted
- *     sequences within gpu_kv_pages; at most max_decode_seqs admitted; at most
- *     swap_in_group per iteration, 0 = no limit, so that decoding can begin
+ *     sequences within gpu_kv_pages; at most max_decode_seqs admitted, and on a
+ *     shard in 8 bits its max_seqs; at most swap_in_group per iteration, 0 = no limit, so that decoding can begin
  *     while the rest of the store is still on its way) its swap-in is requested; every sequence on board gets one token; finished
  *     ones free their pages.  When the store is empty and nothing is arriving:
  *     back to prefilling if requests wait (sequences still decoding keep their

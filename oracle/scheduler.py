@@ -24,7 +24,7 @@ so that two implementations can be compared action by action):
   * batch formation: requests are served in arrival order; a prefill batch takes
     requests while the sum of prompt lengths stays within `max_prefill_tokens`
     (a longer single prompt forms a batch of its own) and the pages of its prompts fit the
-    GPU store;
+    GPU store, and its prompts' number the sequences that store has room for;
   * "full": the next request's prompt does not fit in what is left of the CPU
     store (capacity counted in tokens; the store is empty whenever a prefill
     phase starts, so there is no fragmentation);
@@ -53,8 +53,9 @@ def pages_of(tokens, page_size=16):
 
 
 def simulate(prompt_lens, out_lens, tier_tokens, gpu_pages, max_prefill_tokens, max_decode_seqs, page_size=16,
-             swap_in_group=0):
-    """Returns (trace, stats).  trace is a list of (code, [request ids]):
+             swap_in_group=0, prefill_seqs=None, decode_seqs=None):
+    """`prefill_seqs`, `decode_seqs`: sequences that the GPU store of either strategy has room for, where that is bounded (caches in 8
+    bits); prompts of earlier batches make room as soon as a batch needs it.  Returns (trace, stats).  trace is a list of (code, [request ids]):
     PREFILL batch, TO_DECODE [], SWAP_IN requested, DECODE step over the ids,
     TO_PREFILL [], FINISH ids (after the action that produced their last token)."""
     n = len(prompt_lens)
@@ -67,6 +68,9 @@ def simulate(prompt_lens, out_lens, tier_tokens, gpu_pages, max_prefill_tokens, 
             raise ValueError("request %d does not fit the GPU store" % i)
         if pages_of(prompt_lens[i], page_size) > gpu_pages:
             raise ValueError("prompt %d does not fit the GPU store" % i)
+    prefill_seqs = n if prefill_seqs is None else prefill_seqs
+    if decode_seqs is not None:
+        max_decode_seqs = min(max_decode_seqs, decode_seqs)
     trace = []
     waiting = list(range(n))            # arrival order
     store = []                          # CPU store, first in first out
@@ -95,6 +99,8 @@ def simulate(prompt_lens, out_lens, tier_tokens, gpu_pages, max_prefill_tokens, 
                 if batch and tokens + prompt_lens[r] > max_prefill_tokens:
                     break
                 if batch and pages + pages_of(prompt_lens[r], page_size) > gpu_pages:
+                    break
+                if batch and len(batch) >= prefill_seqs:
                     break
                 waiting.pop(0)
                 batch.append(r)

@@ -118,6 +118,7 @@ def load_library():
         "ss_kv8_attn_prefill": (I, [V, D, I, P(_Batch), P(_Qkv), V, V]),
         "ss_kv8_attn_decode": (I, [V, D, I, P(_Batch), P(_Qkv), V, V]),
         "ss_kv8_weights": (I, [V, D, I, P(L), I, V, V]),
+        "ss_kv8_free_seqs": (L, [V, D]),
         "ss_kv8_weights_len": (I, [V, D, P(L), I, P(L)]),
         "ss_kv8_evict": (I, [V, D, P(L), P(C.c_int32), I, I, V]),
         "ss_kv_page_table": (I, [V, D, L, P(C.c_int32), P(C.c_int32)]),
@@ -148,7 +149,7 @@ def load_library():
 EXPORTED = ("ss_create ss_destroy ss_last_error ss_load_layer ss_host_weights_put ss_reshard_weights ss_weights_wait "
             "ss_weights_shard_bytes ss_weights_read ss_layer_prefill ss_layer_decode ss_layers_prefill ss_layers_decode ss_kv_swap "
             "ss_kv_reshard ss_sync ss_kv_jobs_issued ss_kv_wait ss_kv_free ss_host_tier_release ss_kv_export_dev ss_kv_import_dev "
-            "ss_kv8_enable ss_kv8_write ss_kv8_attn_prefill ss_kv8_attn_decode ss_kv8_weights ss_kv8_weights_len ss_kv8_evict "
+            "ss_kv8_enable ss_kv8_write ss_kv8_attn_prefill ss_kv8_attn_decode ss_kv8_weights ss_kv8_weights_len ss_kv8_evict ss_kv8_free_seqs "
             "ss_kv_page_table ss_kv_seq_len ss_kv_read ss_host_tier_read ss_host_tier_used_bytes "
             "ss_kv_free_pages ss_load_head ss_embed ss_lm_head ss_lm_head_noalloc ss_get_config ss_offline_run ss_prof_enable ss_prof_read ss_prof_reset").split()
 
@@ -409,6 +410,12 @@ class Context:
             raise ValueError("%d sequences, %d lengths to keep" % (len(s), len(k)))
         self._ck(self.lib.ss_kv8_evict(self.h, C.byref(desc), _p(s),
                                        _p(k), len(s), recent, stream))
+
+    def kv8_free_seqs(self, desc):
+        n = self.lib.ss_kv8_free_seqs(self.h, C.byref(desc))
+        if n < 0:
+            self._ck(int(n))
+        return n
 
     # ---- inspection
     def kv_page_table(self, desc, seq):

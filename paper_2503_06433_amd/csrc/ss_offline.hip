@@ -5,20 +5,21 @@
 //
 // The policy, as deterministic rules (the paper fixes the triggers, the rest is this library's reading):
 //   prefill stage   requests in arrival order; a batch takes requests while the prompt tokens stay within
-//                   max_prefill_tokens (a longer prompt alone) and the prompts' pages fit the GPU store; the
-//                   cache of every batch is swapped out to the CPU store behind the batch; the stage ends when
+//                   max_prefill_tokens (a longer prompt alone) and the prompts' pages fit the GPU store (a cache in
+//                   8 bits: their number what it has room for); the cache of every batch is swapped out to the CPU store behind the batch; the stage ends when
 //                   the next prompt does not fit in the store ("full") or nothing is left to prefill.  A request that wants a single token is
 //                   finished by its prefill and never enters the store.
 //   decode stage    per iteration: (1) the caches requested in the previous iteration come on board;
 //                   (2) while the head of the store fits (pages of its final length next to those promised
-//                   to admitted sequences, at most max_decode_seqs admitted, at most swap_in_group per
-//                   iteration) its swap-in is requested;
+//                   to admitted sequences, at most max_decode_seqs and what a cache in 8 bits has room for
+//                   admitted, at most swap_in_group per iteration) its swap-in is requested;
 //                   (3) one token for every sequence on board; finished ones leave and free their pages;
 //                   (4) when the store is empty and nothing is arriving: back to prefilling if requests are
 //                   waiting (sequences still decoding keep their pages and continue in the next decode
 //                   stage), else on until all are finished.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <chrono>
 #include <cstdio>
 #include <deque>
@@ -106,6 +107,12 @@ extern "C" int ss_offline_run(ss_ctx* c, const ss_offline_cfg* cfg, int32_t n, c
     const int64_t tok_bytes = (int64_t)2 * m.n_kv_heads * m.head_dim * (int64_t)es * m.n_layers;
     const int64_t tier_tokens = rt.host_tier_bytes / tok_bytes;
     const int64_t gpu_pages = rt.gpu_kv_pages;
+    // a cache in 8 bits has room for a number of sequences; others only for pages
+    auto seqs_left = [&](const ss_shard_desc& d) {
+        const int64_t k = ss_kv8_free_seqs(c, &d);
+        return k < 0 ? (int64_t)INT32_MAX : k;
+    };
+    const int64_t p_seqs = seqs_left(P), d_seqs = std::min<int64_t>(seqs_left(D), cfg->max_decode_seqs);
     auto pages_of = [&](int64_t tokens) { return (tokens + ps - 1) / ps; };
     auto final_pages = [&](int r) { return pages_of((int64_t)prompt_lens[r] + out_lens[r] - 1); };
     std::vector<int64_t> p_off(n + 1, 0), o_off(n + 1, 0);
@@ -199,7 +206,7 @@ extern "C" int ss_offline_run(ss_ctx* c, const ss_offline_cfg* cfg, int32_t n, c
                 const int64_t need = out_lens[r] > 1 ? prompt_lens[r] : 0;
                 if (store_used + need > tier_tokens) { full = true; break; }
                 if (!batch.empty() && tokens + prompt_lens[r] > cfg->max_prefill_tokens) break;
-                if (!batch.empty() && need_pages + pages_of(prompt_lens[r]) > gpu_pages) break;
+                if (!batch.empty() && (need_pages + pages_of(prompt_lens[r]) > gpu_pages || (int64_t)batch.size() >= p_seqs)) break;
                 waiting.pop_front();
                 batch.push_back(r);
                 tokens += prompt_lens[r];
@@ -207,8 +214,8 @@ extern "C" int ss_offline_run(ss_ctx* c, const ss_offline_cfg* cfg, int32_t n, c
                 store_used += need;
             }
             if (batch.empty()) break;
-            // pages for the batch: earlier batches give theirs back once their swap-out has read them
-            while (!out_batches.empty() && ss_kv_free_pages(c, &P) < need_pages) {
+            // room for the batch: earlier batches give theirs back once their swap-out has read it
+            while (!out_batches.empty() && (ss_kv_free_pages(c, &P) < need_pages || seqs_left(P) < (int64_t)batch.size())) {
                 OFF_TRY(free_ids(P, out_batches.front()));
                 out_batches.pop_front();
             }
@@ -258,7 +265,7 @@ extern "C" int ss_offline_run(ss_ctx* c, const ss_offline_cfg* cfg, int32_t n, c
             }
             std::vector<int> asked;
             while (!store.empty() && promised + final_pages(store.front()) <= gpu_pages &&
-                   (int)(running.size() + asked.size()) < cfg->max_decode_seqs &&
+                   (int64_t)(running.size() + asked.size()) < d_seqs &&
                    (cfg->swap_in_group <= 0 || (int)asked.size() < cfg->swap_in_group)) {
                 const int r = store.front();
                 store.pop_front();

@@ -3133,6 +3133,14 @@ int ss_host_tier_read(ss_ctx* c, int64_t seq, int layer, void* host_out) {
 
 int64_t ss_host_tier_used_bytes(ss_ctx* c) { return c ? (int64_t)c->tier_used : -1; }
 
+int64_t ss_kv8_free_seqs(ss_ctx* c, const ss_shard_desc* d) {
+    if (!c) return SS_EINVAL;
+    Shard* s = nullptr;
+    int rc = kv8_shard(c, d, &s);
+    if (rc) return rc;
+    return s->pools_ready ? (int64_t)s->free_slots.size() : s->kv8_slots;
+}
+
 int64_t ss_kv_free_pages(ss_ctx* c, const ss_shard_desc* d) {
     if (!c) return SS_EINVAL;
     Shard* s = nullptr;
