@@ -1,8 +1,9 @@
 // Cache in 8 bits: what fills it, reads it back, keeps the accumulated attention weights and evicts by them.  Everything here moves
-// data: bound by HBM (32 prompts of 512 - 4096 tokens on 8 heads written in 107 us, 4.3 TB/s, and read back in 82, 5.6 TB/s).  The arithmetic of a block (see Kv8Layer): A = max |v|, q = rint(v * 127 / A).  The product v * 127 is exact
-// for 16-bit v and the quotient is correctly rounded; a quotient of two numbers of up to 11 bits is never closer to half a
-// step than 2^-12 without being on it, the error of the fp32 quotient is at most 2^-18: q is the one of real arithmetic.  For 32-bit v
-// a quotient that close to half a step is formed again in 64 bits (25 bits decide there).
+// data: bound by HBM (32 prompts of 512 - 4096 tokens on 8 heads written in 107 us, 4.3 TB/s, and read back in 82, 5.6 TB/s).
+// The arithmetic of a block (see Kv8Layer): A = max |v|, q = rint(v * 127 / A).  For 16-bit v the product v * 127 is exact, the quotient
+// correctly rounded, and q the one of real arithmetic: with whole numbers m, M < 2^11 for v = m 2^-j (j >= 0) and A = M >= 2^10, the quotient
+// is (254 m - (2 k + 1) M 2^j) / (2 M 2^j) away from half a step k + 1 / 2, which is 0 or more than 2^-(12 + j); it is below 2^(8 - j), so its
+// rounding moves it by 2^-(16 + j) at most.  For 32-bit v a quotient close to half a step is formed again in 64 bits (25 bits decide there).
 #include "ss_device.h"
 #include "ss_kernels.h"
 
