@@ -232,7 +232,7 @@ int ss_kv_import_dev(ss_ctx*, const ss_shard_desc*, const int64_t* seq_ids, cons
 
 /* ---- KV caches in 8 bits ---------------------------------------------------
  * The KV store bounds how many sequences decode at once (paper section 4.2, b_max in Appendix A.3), and its bytes
- * bound a decode step.  A shard can keep its pages in 8 bits: half the store, half the bytes.
+ * bound a decode step.  A shard can keep its pages in 8 bits: half the store, half the bytes (the host tier keeps the model dtype).
  *
  * A block is 16 consecutive cached tokens of one kv head, K and V apart: one page's share of a head.  A full block whose
  * largest magnitude is A holds the whole numbers q = v * 127 / A, rounded to the nearest, halves to even, and stands

@@ -504,7 +504,7 @@ static void launch_decode(const void* q, int64_t q_stride, void* out, int n_q, i
 // wave widening its own operands would cost 1.5 times the vector operations of the softmax).  The whole numbers stay as they are: K's
 // step goes into the exponent's factor, V's into the weight (v_step).  Two stages: while one is multiplied, the next is
 // widened from registers and the one behind it requested.
-// 24 prompts of 512 - 4096 tokens, 64 heads on 8: 3.1 ms, 890 TFLOP/s of the 1190 of a large product.  A tile takes a block some 2 us, of which
+// 24 prompts of 512 - 4096 tokens, 64 heads on 8: 3.0 - 3.3 ms with the clock, 830 - 920 TFLOP/s; a large product reaches 1240 - 1380.  A tile takes a block some 2 us, of which
 // the matrix cores work 0.85 and the vector units (exponentials, maxima, sums, conversions) about as long; they overlap in part.
 // Not better: the two waves of a SIMD half a tile apart, with a barrier a phase (the vector phase alone takes 2300 cycles), priorities,
 // 64 rows a wave and all fragments in registers in front of the products (both spill).
