@@ -548,6 +548,7 @@ int ensure_pools8(ss_ctx* c, Shard* s) {
     if (e == hipSuccess) e = hipMemcpy(d, layers.data(), sizeof(ssk::Kv8Layer) * layers.size(), hipMemcpyHostToDevice);
     if (e != hipSuccess) {
         for (void* p : mem) (void)hipFree(p);
+        (void)hipGetLastError();                 // reported here, not by the next launch
         return fail(c, e == hipErrorOutOfMemory ? SS_ENOMEM : SS_EHIP, "cache in 8 bits: %s", hipGetErrorString(e));
     }
     s->kv8_layers = std::move(layers);

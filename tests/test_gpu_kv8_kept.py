@@ -90,6 +90,18 @@ def test_an_allocation_that_failed_does_not_fail_the_next_call():
     assert np.isfinite(one(101)).all()
 
 
+def test_a_cache_that_the_card_does_not_hold():
+    """A terabyte of pages: the call that would allocate them says so, and nothing that follows is told of it."""
+    rng = np.random.default_rng(63)
+    c, small = (Cache(wl.BF16, 1, 1, 64, pages=p, seqs=1) for p in (1 << 30, 4))
+    k = c.tokens(rng, 5, 1)[1]
+    small.ctx.kv8_write(small.desc, 0, [0], [5], [0], k, k)
+    for _ in range(2):
+        _out_of_memory(lambda: c.ctx.kv8_write(c.desc, 0, [0], [5], [0], k, k))
+    got = attn(small, 0, [0], [5], [0], k, k, k, False)
+    assert np.isfinite(got).all() and float((k + 1).sum()) == float((k + 1).sum())
+
+
 def test_a_workspace_that_the_card_does_not_hold():
     c, call, one, watched = _too_large()
     before = _state(c, watched)
