@@ -949,12 +949,12 @@ int prepare_batch(ss_ctx* c, Shard* s, const ss_batch* b, bool decode, MetaSlot*
     ms.wk.item_order = (const int32_t*)(ms.dev + off_iord);
     ms.wk.n_items = (int)n_items;
     ms.wk.max_items_per_seq = max_items;
-    ms.shard = s;
     ms.version = s->version;
     ms.decode = decode;
     ms.seq_ids.assign(b->seq_ids, b->seq_ids + n);
     ms.q_lens.assign(b->q_lens, b->q_lens + n);
     ms.kv_before.assign(b->kv_lens_before, b->kv_lens_before + n);
+    ms.shard = s;                            // last: a key that host memory did not hold is never found
     *out = &ms;
     return SS_OK;
 }
@@ -1412,10 +1412,11 @@ int prepare8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, bool w
     k.pf_items = pf.items.empty() ? nullptr : at(o_pf); k.pf_stride = pf.stride; k.pf_blocks = pf.blocks;
     k.pf_cuts = at(o_pc); k.n_cuts = (int)pf.cuts.size() / 8; k.n_parts = pf.n_parts;
     k.items = at(o_it); k.seq_item0 = at(o_si); k.n_items = n_items; k.max_items_per_seq = max_items;
-    ms->shard = s; ms->version = s->version; ms->decode = decode; ms->write = write; ms->attend = attend;
+    ms->version = s->version; ms->decode = decode; ms->write = write; ms->attend = attend;
     ms->seq_ids.assign(b->seq_ids, b->seq_ids + n);
     ms->q_lens.assign(b->q_lens, b->q_lens + n);
     ms->before = std::move(before); ms->end = std::move(end); ms->pos = std::move(pos);
+    ms->shard = s;                           // last: a key that host memory did not hold is never found
     *out = ms;
     return SS_OK;
 }
