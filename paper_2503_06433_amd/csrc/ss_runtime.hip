@@ -1084,7 +1084,7 @@ int guarded(ss_ctx* c, F f) {
 int refuse_capture(ss_ctx* c, hipStream_t st) {
     hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
     HIP_TRY(c, hipStreamIsCapturing(st, &cap));
-    if (cap != hipStreamCaptureStatusNone) return fail(c, SS_EHIP, "cache in 8 bits: the stream is capturing");
+    if (cap != hipStreamCaptureStatusNone) return fail(c, SS_EHIP, "the stream is capturing: a graph would hold the page lists of now");
     return SS_OK;
 }
 
@@ -1457,8 +1457,7 @@ int run_attn8(ss_ctx* c, Shard* s, int ll, Meta8Slot* ms, bool decode, const voi
 int run_attn_phase8(ss_ctx* c, Shard* s, int ll, const ss_batch* b, bool decode, const void* x_in, void* out, bool residual, hipStream_t st) {
     const ss_model_cfg& m = c->m;
     const LayerW& w = s->w[ll];
-    int rc = refuse_capture(c, st);
-    if (rc) return rc;
+    int rc;
     Taken8 taken;
     Meta8Slot* ms = nullptr;
     if ((rc = prepare8(c, s, ll, b, decode, true, true, &taken, &ms)) || (rc = attn8_ready(c, s, ms, decode))) return rc;
@@ -1541,6 +1540,8 @@ int layer_call(ss_ctx* c, const ss_shard_desc* d, int layer, int phase, const ss
         return fail(c, SS_EINVAL, "layer %d outside the shard's range [%d,%d)", layer, d->layer_begin, d->layer_end);
     const int ll = layer - d->layer_begin;
     if (!s->w[ll].loaded) return fail(c, SS_EINVAL, "layer %d not loaded for this shard", layer);
+    // before anything is allocated, which a capture would not survive
+    if (s->kv8 && (phase & SS_ATTN) && (rc = refuse_capture(c, (hipStream_t)stream))) return rc;
     if (s->w_pending) {      // a reload on the weight stream: the caller's stream waits for it, the host does not
         HIP_TRY(c, hipStreamWaitEvent((hipStream_t)stream, s->w_ready, 0));
         if (hipEventQuery(s->w_ready) == hipSuccess) s->w_pending = false;
@@ -1583,7 +1584,9 @@ int layers_call(ss_ctx* c, const ss_shard_desc* d, const ss_batch* b, const void
     for (int i = 0; i < b->n_seqs; ++i) T += b->q_lens[i];
     if (T <= 0 || T > (1 << 30)) return fail(c, SS_EINVAL, "bad token count");
     const int n = d->layer_end - d->layer_begin;
-    int rc;
+    Shard* s = nullptr;
+    int rc = get_shard(c, d, &s);
+    if (rc || (s->kv8 && (rc = refuse_capture(c, (hipStream_t)stream)))) return rc;
     for (int j = 0; j < (n > 2 ? 2 : n - 1); ++j)
         if ((rc = ensure_buf(c, c->ws_chain[j], (size_t)T * c->m.hidden * c->es))) return rc;
     const void* in = x_in;
@@ -1994,9 +1997,7 @@ void wait_idle(ss_ctx* c) {
 // that reads them: from two page-locked images in turn, each rewritten once the kernels of its last use are through.
 template <class F>
 int over_units(ss_ctx* c, Shard* s, const std::vector<SeqJob>& seqs, const std::vector<Unit>& units, hipStream_t st, F fn) {
-    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;         // a captured graph cannot hold the call: the page
-    HIP_TRY(c, hipStreamIsCapturing(st, &cap));                      // lists are those of now
-    if (cap != hipStreamCaptureStatusNone) return fail(c, SS_EHIP, "device-side export / import: the stream is capturing");
+    if (const int rc = refuse_capture(c, st)) return rc;
     wait_idle(c);   // pages that a mover still writes are exported as they will be, pages it still reads not overwritten
     size_t stage_off = 0;
     for (size_t u0 = 0; u0 < units.size(); u0 += 32768) {
@@ -2639,7 +2640,7 @@ static int kv_swap(ss_ctx* c, const ss_shard_desc* d, int dir, const int64_t* se
     if (!c->tier || !c->slot_bytes) return fail(c, SS_EINVAL, "context was created without a host tier / pinned ring");
     Shard* s = nullptr;
     int rc = get_shard(c, d, &s);
-    if (rc) return rc;
+    if (rc || (rc = refuse_capture(c, (hipStream_t)stream))) return rc;
     if ((rc = ensure_pools(c, s))) return rc;
     if (n == 0) return SS_OK;
     Job job;
@@ -2801,6 +2802,8 @@ static int xfer_dev(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, c
     Shard* s = nullptr;
     int rc = get_shard(c, d, &s);
     if (rc) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    if ((rc = refuse_capture(c, st))) return rc;
     if ((rc = ensure_pools(c, s))) return rc;
     if (n == 0) return SS_OK;
     std::vector<SeqJob> seqs;
@@ -2829,10 +2832,10 @@ static int xfer_dev(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, c
         }
     }
     const std::vector<Unit> units = make_units(c, s, seqs);
-    hipStream_t st = (hipStream_t)stream;
-    return over_units(c, s, seqs, units, st, [&](const ssk::RepackUnits& ru, size_t off) {
+    rc = over_units(c, s, seqs, units, st, [&](const ssk::RepackUnits& ru, size_t off) {
         return repack(c, s, import, ru, (uint8_t*)staging + off, st);
     });
+    return rc;
 }
 
 int ss_kv_export_dev(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, int n, void* staging, void* stream) {

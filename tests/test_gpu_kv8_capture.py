@@ -1,0 +1,101 @@
+"""Calls on a capturing stream are refused before they allocate or enter anything: the capture goes on, and the shard is as it was."""
+import numpy as np
+import pytest
+
+import workloads as wl
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+if torch.cuda.is_available():
+    import paper_2503_06433_amd as ss
+    from paper_2503_06433_amd import harness as hz
+    from paper_2503_06433_amd.harness import make_context, pp_desc, tp_desc, to_device
+
+
+def test_first_calls_of_a_shard_under_capture():
+    cfg = wl.ModelCfg(hidden=512, n_q_heads=4, n_kv_heads=2, head_dim=64, ffn=512, n_layers=1, dtype=wl.BF16)
+    _, raws = wl.make_layer_weights(cfg, 5)
+    ctx = make_context(cfg, pages=16, tier_bytes=1 << 20, pinned_bytes=1 << 20)
+    p, t = pp_desc(cfg), tp_desc(cfg, 1, 0)
+    for d in (p, t):
+        ctx.kv8_enable(d, max_seqs=4, weights=True)
+        ctx.load_layer(d, 0, raws)
+    _, xr = wl.make_activations((20, cfg.hidden), 7, wl.BF16)
+    x = to_device(xr, wl.BF16)
+    out, mark = hz.empty_like_acts(20, cfg.hidden, wl.BF16), torch.zeros(4, device="cuda")
+    k = torch.randn(20, 2, 64, device="cuda").to(torch.bfloat16)
+    q, a, w = (torch.zeros(20, 4, 64, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+    stage = torch.randn(2 * 20 * 2 * 64, device="cuda").to(torch.bfloat16)
+    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    st = s.cuda_stream
+    torch.cuda.synchronize()
+
+    def refused(call):
+        with pytest.raises(ss.SeesawError) as e:
+            call()
+        assert e.value.code == ss.SS_EHIP and "captur" in str(e.value)
+
+    with torch.cuda.graph(g, stream=s):
+        refused(lambda: ctx.layer_prefill(p, 0, ss.SS_BOTH, [0], [20], [0], x, out, st))
+        refused(lambda: ctx.layer_prefill(p, 0, ss.SS_ATTN, [0], [20], [0], x, out, st))
+        refused(lambda: ctx.layer_decode(p, 0, ss.SS_BOTH, [0], [0], x, out, st))
+        refused(lambda: ctx.layers_prefill(p, [0], [20], [0], x, out, st))
+        refused(lambda: ctx.layers_decode(p, [0], [0], x, out, st))
+        refused(lambda: ctx.kv8_write(p, 0, [0], [20], [0], k, k, st))
+        refused(lambda: ctx.kv8_attn_prefill(p, 0, [0], [20], [0], q, k, k, a, st))
+        refused(lambda: ctx.kv8_attn_decode(p, 0, [0], [0], q[:1], k[:1], k[:1], a[:1], st))
+        refused(lambda: ctx.kv_import_dev(p, [0], [20], stage, st))
+        refused(lambda: ctx.kv_swap(p, ss.SS_OUT, [0], st))
+        refused(lambda: ctx.kv_reshard(p, t, [0], st))
+        refused(lambda: ctx.kv8_evict(p, [], [], 0, st))
+        mark.add_(1)
+    for i in range(3):                                      # the graph holds what was captured beside them
+        g.replay()
+        torch.cuda.synchronize()
+        assert (mark == i + 1).all()
+        if i == 0:                                          # nothing was entered: the same calls go through
+            ctx.kv_import_dev(p, [0], [20], stage)
+            ctx.kv_reshard(p, t, [0])
+            ctx.sync()
+            assert ctx.kv_seq_len(t, 0) == 20 and ctx.kv8_free_seqs(p) == 3
+            ctx.layer_prefill(p, 0, ss.SS_BOTH, [1], [20], [0], x, out)
+            torch.cuda.synchronize()
+            assert np.isfinite(hz.to_f64(out, wl.BF16)).all()
+    # and with everything there already
+    g2 = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g2, stream=s):
+        refused(lambda: ctx.kv_export_dev(p, [0], stage, st))
+        refused(lambda: ctx.kv8_weights(p, ss.SS_OUT, [0], torch.empty(40, device="cuda"), st))
+        refused(lambda: ctx.kv8_evict(p, [0], [16], 4, st))
+        refused(lambda: ctx.layer_decode(p, 0, ss.SS_BOTH, [0], [20], x, out, st))
+        mark.add_(1)
+    g2.replay()
+    torch.cuda.synchronize()
+    assert (mark == 4).all() and ctx.kv_seq_len(p, 0) == 20
+    ctx.destroy()
+
+
+@pytest.mark.parametrize("eight", [True, False])
+def test_imports_that_are_refused_leave_nothing_behind(eight):
+    cfg = wl.ModelCfg(hidden=512, n_q_heads=4, n_kv_heads=2, head_dim=64, ffn=512, n_layers=1, dtype=wl.F16)
+    ctx = make_context(cfg, pages=16)
+    p = pp_desc(cfg)
+    if eight:
+        ctx.kv8_enable(p, max_seqs=2)
+    stage = torch.randn(2 * 30 * 2 * 64, device="cuda").to(torch.float16)
+    ctx.kv_import_dev(p, [7], [10], stage)
+    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    free = ctx.kv_free_pages(p)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=s):
+        with pytest.raises(ss.SeesawError) as e:
+            ctx.kv_import_dev(p, [8], [20], stage, s.cuda_stream)
+        stage[:1].add_(0)
+    assert e.value.code == ss.SS_EHIP and ctx.kv_free_pages(p) == free
+    with pytest.raises(ss.SeesawError):
+        ctx.kv_seq_len(p, 8)
+    ctx.kv_import_dev(p, [8], [20], stage)
+    torch.cuda.synchronize()
+    assert ctx.kv_seq_len(p, 8) == 20
+    ctx.destroy()
