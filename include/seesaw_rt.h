@@ -28,7 +28,8 @@
  *     come after; they may be any stream.
  *   - ss_kv_swap(SS_IN) and ss_kv_import_dev are all or nothing: when the pages
  *     of the listed sequences do not fit the pool together, SS_ENOMEM is
- *     returned, no page is taken and no sequence becomes resident.
+ *     returned, no page is taken and no sequence becomes resident; an import
+ *     that fails for another reason leaves none behind either.
  */
 #ifndef SEESAW_RT_H
 #define SEESAW_RT_H
@@ -225,7 +226,7 @@ int ss_host_tier_release(ss_ctx*, const int64_t* seq_ids, int n);
  * buffer laid out [seq][layer_local][K|V][head_local][position][head_dim],
  * sequences back to back at exact lengths, model dtype.  Export gathers pages
  * into it; import allocates pages for (seq_ids, lens) and scatters into them.
- * Both run on `stream`. */
+ * Both run on `stream`, which may not be capturing, like that of the swaps (SS_EHIP). */
 int ss_kv_export_dev(ss_ctx*, const ss_shard_desc*, const int64_t* seq_ids, int n, void* staging, void* stream);
 int ss_kv_import_dev(ss_ctx*, const ss_shard_desc*, const int64_t* seq_ids, const int32_t* lens, int n,
                      const void* staging, void* stream);

@@ -2835,6 +2835,14 @@ static int xfer_dev(ss_ctx* c, const ss_shard_desc* d, const int64_t* seq_ids, c
     rc = over_units(c, s, seqs, units, st, [&](const ssk::RepackUnits& ru, size_t off) {
         return repack(c, s, import, ru, (uint8_t*)staging + off, st);
     });
+    if (rc && import) {                          // what did not come whole does not stay
+        for (const SeqJob& sj : seqs) {
+            for (int32_t p : sj.pages) s->free_pages.push(p);
+            if (sj.slot >= 0) s->free_slots.push(sj.slot);
+            s->seqs.erase(sj.seq);
+        }
+        s->version++;
+    }
     return rc;
 }
 

@@ -99,3 +99,27 @@ def test_imports_that_are_refused_leave_nothing_behind(eight):
     torch.cuda.synchronize()
     assert ctx.kv_seq_len(p, 8) == 20
     ctx.destroy()
+
+
+@pytest.mark.parametrize("eight", [True, False])
+def test_an_import_whose_page_lists_do_not_fit_leaves_nothing_behind(eight):
+    """34 million tokens of one head in one call: more page numbers than an image of lists holds."""
+    n = 34_000_000
+    cfg = wl.ModelCfg(hidden=64, n_q_heads=1, n_kv_heads=1, head_dim=64, ffn=64, n_layers=1, dtype=wl.BF16)
+    ctx = make_context(cfg, pages=n // 16 + 8)
+    p = pp_desc(cfg)
+    if eight:
+        ctx.kv8_enable(p, max_seqs=2)
+    stage = torch.zeros(2 * n * 64, device="cuda", dtype=torch.bfloat16)
+    ctx.kv_import_dev(p, [7], [40], stage)
+    free = ctx.kv_free_pages(p)
+    for _ in range(2):
+        with pytest.raises(ss.SeesawError) as e:
+            ctx.kv_import_dev(p, [8], [n], stage)
+        assert e.value.code == ss.SS_ENOMEM and ctx.kv_free_pages(p) == free
+        with pytest.raises(ss.SeesawError):
+            ctx.kv_seq_len(p, 8)
+    ctx.kv_import_dev(p, [8], [100], stage)
+    torch.cuda.synchronize()
+    assert ctx.kv_seq_len(p, 8) == 100
+    ctx.destroy()
