@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -10,6 +11,14 @@ if ROOT not in sys.path:
 
 def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a real MI355X (run with -m gpu)")
+
+
+@pytest.fixture(autouse=True, scope="module")
+def _contexts_end_with_their_module():
+    """A context that an expected error still refers to (the error holds its frame, a cycle) keeps its device memory until the collector
+    comes by: not in the middle of another module's captures or measurements of free memory."""
+    yield
+    gc.collect()
 
 
 def pytest_terminal_summary(terminalreporter):

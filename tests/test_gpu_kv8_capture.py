@@ -1,4 +1,7 @@
 """Calls on a capturing stream are refused before they allocate or enter anything: the capture goes on, and the shard is as it was."""
+import contextlib
+import gc
+
 import numpy as np
 import pytest
 
@@ -11,6 +14,20 @@ if torch.cuda.is_available():
     import paper_2503_06433_amd as ss
     from paper_2503_06433_amd import harness as hz
     from paper_2503_06433_amd.harness import make_context, pp_desc, tp_desc, to_device
+
+
+@contextlib.contextmanager
+def _capturing(graph, stream):
+    """Contexts of other tests that wait in reference cycles (exceptions hold their frames) free device memory when they are collected,
+    which a capture does not survive: not in here."""
+    gc.collect()
+    torch.cuda.synchronize()
+    gc.disable()
+    try:
+        with torch.cuda.graph(graph, stream=stream):
+            yield
+    finally:
+        gc.enable()
 
 
 def test_first_calls_of_a_shard_under_capture():
@@ -36,7 +53,7 @@ def test_first_calls_of_a_shard_under_capture():
             call()
         assert e.value.code == ss.SS_EHIP and "captur" in str(e.value)
 
-    with torch.cuda.graph(g, stream=s):
+    with _capturing(g, s):
         refused(lambda: ctx.layer_prefill(p, 0, ss.SS_BOTH, [0], [20], [0], x, out, st))
         refused(lambda: ctx.layer_prefill(p, 0, ss.SS_ATTN, [0], [20], [0], x, out, st))
         refused(lambda: ctx.layer_decode(p, 0, ss.SS_BOTH, [0], [0], x, out, st))
@@ -64,7 +81,7 @@ def test_first_calls_of_a_shard_under_capture():
             assert np.isfinite(hz.to_f64(out, wl.BF16)).all()
     # and with everything there already
     g2 = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(g2, stream=s):
+    with _capturing(g2, s):
         refused(lambda: ctx.kv_export_dev(p, [0], stage, st))
         refused(lambda: ctx.kv8_weights(p, ss.SS_OUT, [0], torch.empty(40, device="cuda"), st))
         refused(lambda: ctx.kv8_evict(p, [0], [16], 4, st))
@@ -88,7 +105,7 @@ def test_imports_that_are_refused_leave_nothing_behind(eight):
     s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
     free = ctx.kv_free_pages(p)
     torch.cuda.synchronize()
-    with torch.cuda.graph(g, stream=s):
+    with _capturing(g, s):
         with pytest.raises(ss.SeesawError) as e:
             ctx.kv_import_dev(p, [8], [20], stage, s.cuda_stream)
         stage[:1].add_(0)
